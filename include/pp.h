@@ -286,6 +286,120 @@ int pp_decode_step(const pp_attn_params* params, const int32_t* lengths, int32_t
                    void* workspace, void* host_workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * A KV cache in pages -- for generation (Section 7) over caches that grow at different speeds, are given back at different
+ * times, or begin with the same rows. The paper has no counterpart. Two pools hold pages of page_size rows; row p of prompt i is
+ * row p % page_size of page page_table[i * table_stride + p / page_size]. The table and everything else that changes
+ * from step to step lives in device memory and is read when the kernels run, so a captured graph goes on working while
+ * prompts grow.
+ *   k_pages, v_pages   device, 16-byte aligned; element d of row r of KV head h of page g at
+ *                      g * page_stride + h * head_stride + r * row_stride + d (elements; one set of strides for both pools):
+ *                      [page, head, row, D] and [page, row, head, D] alike. Strides are multiples of 16 bytes, at least D, and
+ *                      no two rows may overlap.
+ *   k_scale, v_scale   device float [Hkv], for PP_CACHE_E4M3 (NULL otherwise): a stored number stands for itself times
+ *                      the scale of its KV head. Finite, above 0.
+ *   page_table         device int32 [k, table_stride]. Entries of rows that a prompt does not have are not used, whatever they hold.
+ *   n_pages            pages of either pool. An entry outside 0 .. n_pages - 1 where a row is needed is not followed:
+ *                      the call sets the status word (PP_PAGED_*) and that prompt's results are unspecified.
+ *   page_size          16, 32, 64, 128 or 256
+ */
+enum { PP_CACHE_BF16 = 0, PP_CACHE_E4M3 = 1 };
+
+typedef struct pp_paged_cache {
+  void* k_pages;
+  void* v_pages;
+  const float* k_scale;
+  const float* v_scale;
+  const int32_t* page_table;
+  int64_t page_stride, head_stride, row_stride;
+  int32_t n_pages, page_size, table_stride;
+  int32_t type;          /* PP_CACHE_* */
+} pp_paged_cache;
+
+/* What the kernels of the paged calls leave in *device_status (the first of them to find something wrong). */
+enum {
+  PP_PAGED_BAD_PROMPT = 201,   /* pp_paged_append: a prompt index >= n_prompts: its row was skipped                     */
+  PP_PAGED_BAD_POSITION = 202, /* pp_paged_append: a position < 0 or past the prompt's table row: its row was skipped   */
+  PP_PAGED_BAD_PAGE = 203,     /* a page table entry outside 0 .. n_pages - 1 where a row is needed                     */
+  PP_PAGED_BAD_LENGTH = 204,   /* a length past the prompt's table row (or at its end, with a token to append): the
+                                  prompt was taken for one of length -1                                                */
+  PP_PAGED_BAD_GROUPS = 205    /* group_ptr does not ascend within 0 .. k: nothing was shared                           */
+};
+
+/*
+ * Rows into a paged cache: row r of k_new and v_new goes to row position[r] of prompt[r], its key rotated by position[r] on
+ * the way (RESTART-PE, Section 3.2, as in pp_prefill_attention), or as it is with PP_FLAG_SKIP_ROPE (keys that the
+ * prefill has rotated: with that flag the call is UNPACK into pages). Rows may come in any order, from one prompt or many.
+ *   params       n_kv_heads, head_dim, rope_base and flags (0 or PP_FLAG_SKIP_ROPE) are read
+ *   prompt       device int32 [n_rows]; a row of no prompt (< 0), such as the padding of a bin, is skipped
+ *   position     device int32 [n_rows] (ignored where prompt < 0)
+ *   n_rows       >= 0; 0 does nothing
+ *   n_prompts    rows of the page table, >= 1
+ *   k_new, v_new device bf16, row r at r * k_stride / r * v_stride elements, [Hkv, D] within a row; a stride of 0 stands for
+ *                Hkv * D, others are multiples of 8 and at least that, so that both may be slices of one projection
+ *   device_status device int32 or NULL, see PP_PAGED_*; the caller zeroes and reads it
+ * Arithmetic: rotation in fp32 with one rounding, to bf16 or, after a division by the scale, to e4m3 (to nearest, what is beyond
+ * its range to +-448, a NaN stays one); the bf16 keys are bit for bit those of the prefill. Two rows of the same prompt and
+ * position in one call leave any mixture of the two. A row may be appended again. Asynchronous on `stream`.
+ * Errors: PP_ERR_INVALID_ARG, PP_ERR_UNSUPPORTED (head_dim, page_size, type, device), PP_ERR_ALIGNMENT, PP_ERR_CUDA.
+ */
+int pp_paged_append(const pp_attn_params* params, const pp_paged_cache* cache, const int32_t* prompt,
+                    const int32_t* position, int64_t n_rows, int32_t n_prompts,
+                    const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride,
+                    int32_t* device_status, void* stream);
+
+/*
+ * pp_decode_step over a paged cache: one generation step for up to 8192 prompts.
+ * With k_new and v_new: the new token of prompt i sits at position lengths[i]; its query and key are rotated by that position,
+ * key and value are appended at row lengths[i], and the query attends to rows 0 .. lengths[i], as the pages hold them.
+ * With both NULL: the pages hold the token already. The query sits at position lengths[i] - 1 and attends to rows
+ * 0 .. lengths[i] - 1; a prompt of length 0 attends to nothing and gets zeros.
+ * A length below 0 marks a row of no prompt (a batch padded to the size of a captured graph): its row of o is not
+ * written, its tensors and its row of the table are not looked at.
+ *   params       as for pp_decode_step; flags must be 0
+ *   lengths      device int32 [k], read when the kernels run and not changed by them
+ *   q_new, k_new, v_new  device bf16, [Hq, D] / [Hkv, D] within a row, strides of rows as in pp_paged_append
+ *   o            device [k, Hq, D] bf16 out
+ *   workspace    device, >= pp_paged_decode_workspace_bytes(params, k, 0), 256-byte aligned; nothing in it has to survive from one
+ *                call to the next, and calls (and graphs) whose work may overlap need one each
+ *   device_status device int32 or NULL, see PP_PAGED_*; the caller zeroes and reads it
+ * No host memory is read after the call and nothing depends on the lengths but what the kernels do: the call can be
+ * captured once and replayed for every step. Two prompts may share pages only below both of their lengths.
+ * Arithmetic: scores, probabilities and sums in fp32 (the rotated query and the probabilities reach the tensor cores as
+ * the sum of two or three 16-bit numbers), one rounding of O to bf16. Cached values may be infinite or NaN; rows that a
+ * prompt does not have may hold anything. Asynchronous on `stream`.
+ * Errors: PP_ERR_INVALID_ARG, PP_ERR_UNSUPPORTED (head_dim, more than 8 query heads per KV head, page_size, type, device),
+ * PP_ERR_TOO_LARGE (k > 8192), PP_ERR_ALIGNMENT, PP_ERR_BUFFER_TOO_SMALL, PP_ERR_CUDA.
+ */
+size_t pp_paged_decode_workspace_bytes(const pp_attn_params* params, int32_t k, int32_t n_groups);
+int pp_paged_decode_step(const pp_attn_params* params, const pp_paged_cache* cache, const int32_t* lengths, int32_t k,
+                         const void* q_new, int64_t q_stride, const void* k_new, int64_t k_stride,
+                         const void* v_new, int64_t v_stride, void* o,
+                         void* workspace, size_t workspace_bytes, int32_t* device_status, void* stream);
+
+/*
+ * pp_paged_decode_step for prompts in groups that begin with the same pages (samples of one prompt, prompts behind one system
+ * prompt): those pages are read once for a group, its prompts' queries side by side on the tensor cores. The result
+ * is that of pp_paged_decode_step up to rounding.
+ *   group_ptr    device int32 [n_groups + 1], ascending within 0 .. k: group g is prompts group_ptr[g] .. group_ptr[g + 1] - 1;
+ *                prompts before the first and behind the last group share nothing
+ *   shared_len   device int32 [n_groups]: the first shared_len[g] rows of the group's prompts lie in the same pages: the
+ *                first shared_len[g] / page_size (rounded down) entries of their table rows are equal, which the caller
+ *                sees to. Cut to the shortest length in the group and to whole pages; 0 or less shares nothing.
+ *   n_groups     1 .. k
+ *   cache        PP_CACHE_BF16 only
+ *   workspace    >= pp_paged_decode_workspace_bytes(params, k, n_groups)
+ * The shared rows must hold finite values (a value that is not makes every query of the group that reads it NaN or infinite
+ * in that element, whatever its weight). Their probabilities and the queries that meet them are rounded to bf16 as in the prefill.
+ * device_status also reports a wait that gave up, as in pp_prefill_attention. Errors as pp_paged_decode_step; PP_ERR_UNSUPPORTED
+ * for an 8-bit cache.
+ */
+int pp_paged_decode_shared(const pp_attn_params* params, const pp_paged_cache* cache, const int32_t* lengths, int32_t k,
+                           const int32_t* group_ptr, const int32_t* shared_len, int32_t n_groups,
+                           const void* q_new, int64_t q_stride, const void* k_new, int64_t k_stride,
+                           const void* v_new, int64_t v_stride, void* o,
+                           void* workspace, size_t workspace_bytes, int32_t* device_status, void* stream);
+
+/*
  * Whole path from host memory (Algorithm 1 (bin size to UNPACK) for one attention layer), for callers whose
  * tensors live on the host. Every tensor goes up in large contiguous copies, is laid out as the
  * packed batch by device kernels (TENSORIZE, padding rows zeroed), the kernels of pp_prefill_fused

@@ -16,6 +16,9 @@ _lib = None
 PP_FLAG_SKIP_ROPE = 1
 PP_FLAG_ROPE_ONLY = 2
 PP_FLAG_KEEP_ROPE_TABLE = 4
+# Types of the pages of a paged cache, and what the paged calls leave in the status word.
+PP_CACHE_BF16, PP_CACHE_E4M3 = 0, 1
+PP_PAGED_BAD_PROMPT, PP_PAGED_BAD_POSITION, PP_PAGED_BAD_PAGE, PP_PAGED_BAD_LENGTH, PP_PAGED_BAD_GROUPS = range(201, 206)
 # Tables of at most this many int32 words travel as kernel parameters in the independent mode (kInlineInts of the library).
 PARAMETER_TABLE_INTS = 896
 
@@ -36,6 +39,15 @@ class AttnParams(ctypes.Structure):
                 ("n_bins", ctypes.c_int32), ("flags", ctypes.c_int32)]
 
 
+class PagedCache(ctypes.Structure):
+    """Mirror of ``pp_paged_cache``."""
+    _fields_ = [("k_pages", ctypes.c_void_p), ("v_pages", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("page_table", ctypes.c_void_p),
+                ("page_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64), ("row_stride", ctypes.c_int64),
+                ("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32), ("table_stride", ctypes.c_int32),
+                ("type", ctypes.c_int32)]
+
+
 def lib_path() -> str:
     return os.path.join(_PKG_DIR, _LIB_NAME)
 
@@ -51,7 +63,7 @@ def load_library():
                           "(needs nvcc); prepack-b200 has no CPU or PyTorch fallback")
     lib = ctypes.CDLL(path)
     i32p, i64p, vp = ctypes.POINTER(ctypes.c_int32), ctypes.POINTER(ctypes.c_int64), ctypes.c_void_p
-    pp = ctypes.POINTER(AttnParams)
+    pp, pc = ctypes.POINTER(AttnParams), ctypes.POINTER(PagedCache)
     sig = {
         "pp_version": (ctypes.c_int, []),
         "pp_strerror": (ctypes.c_char_p, [ctypes.c_int]),
@@ -75,6 +87,13 @@ def load_library():
         "pp_decode_workspace_bytes": (ctypes.c_size_t, [pp, i32p, ctypes.c_int32]),
         "pp_decode_step": (ctypes.c_int, [pp, i32p, ctypes.c_int32, vp, vp, vp, vp, vp, vp, i64p, i32p, vp, vp,
                                           ctypes.c_size_t, vp]),
+        "pp_paged_append": (ctypes.c_int, [pp, pc, vp, vp, ctypes.c_int64, ctypes.c_int32, vp, ctypes.c_int64, vp,
+                                           ctypes.c_int64, vp, vp]),
+        "pp_paged_decode_workspace_bytes": (ctypes.c_size_t, [pp, ctypes.c_int32, ctypes.c_int32]),
+        "pp_paged_decode_step": (ctypes.c_int, [pp, pc, vp, ctypes.c_int32, vp, ctypes.c_int64, vp, ctypes.c_int64, vp,
+                                                ctypes.c_int64, vp, vp, ctypes.c_size_t, vp, vp]),
+        "pp_paged_decode_shared": (ctypes.c_int, [pp, pc, vp, ctypes.c_int32, vp, vp, ctypes.c_int32, vp, ctypes.c_int64, vp,
+                                                  ctypes.c_int64, vp, ctypes.c_int64, vp, vp, ctypes.c_size_t, vp, vp]),
         "pp_prefill_host_arena_bytes": (ctypes.c_size_t, [pp, i32p, ctypes.c_int32]),
         "pp_prefill_host_groups": (ctypes.c_int32, [ctypes.c_int32]),
         "pp_prefill_host": (ctypes.c_int, [pp, i32p, ctypes.c_int32, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]),
@@ -229,6 +248,31 @@ def pp_decode_step(params: AttnParams, lengths, q_new, k_new, v_new, o, k_cache,
     _check((_native or _load_native()).decode_step(
         params, lengths, q_new, k_new, v_new, o, k_cache, v_cache, cache_off, cache_cap, workspace, host_workspace,
         workspace_bytes, stream), "pp_decode_step")
+
+
+def pp_paged_append(params: AttnParams, cache: PagedCache, prompt, position, n_rows: int, n_prompts: int, k_new, k_stride: int,
+                    v_new, v_stride: int, device_status=None, stream: int = 0) -> None:
+    _check((_native or _load_native()).paged_append(params, cache, prompt, position, n_rows, n_prompts, k_new, k_stride, v_new,
+                                                    v_stride, device_status, stream), "pp_paged_append")
+
+
+def pp_paged_decode_workspace_bytes(params: AttnParams, k: int, n_groups: int = 0) -> int:
+    return int(load_library().pp_paged_decode_workspace_bytes(ctypes.byref(params), k, n_groups))
+
+
+def pp_paged_decode_step(params: AttnParams, cache: PagedCache, lengths, k: int, q_new, q_stride: int, k_new, k_stride: int,
+                         v_new, v_stride: int, o, workspace, workspace_bytes: int, device_status=None, stream: int = 0) -> None:
+    _check((_native or _load_native()).paged_decode(
+        params, cache, lengths, k, None, None, -1, q_new, q_stride, k_new, k_stride, v_new, v_stride, o, workspace,
+        workspace_bytes, device_status, stream), "pp_paged_decode_step")
+
+
+def pp_paged_decode_shared(params: AttnParams, cache: PagedCache, lengths, k: int, group_ptr, shared_len, n_groups: int, q_new,
+                           q_stride: int, k_new, k_stride: int, v_new, v_stride: int, o, workspace, workspace_bytes: int,
+                           device_status=None, stream: int = 0) -> None:
+    _check((_native or _load_native()).paged_decode(
+        params, cache, lengths, k, group_ptr, shared_len, max(n_groups, 0), q_new, q_stride, k_new, k_stride, v_new, v_stride,
+        o, workspace, workspace_bytes, device_status, stream), "pp_paged_decode_shared")
 
 
 def pp_selftest_bounded_wait(device_status, limit_ms: int, stream: int = 0) -> None:

@@ -13,9 +13,9 @@ CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "libprepack_b200.so")
 MODULE_PATH = os.path.join(PKG_DIR, "_native" + sysconfig.get_config_var("EXT_SUFFIX"))
 SOURCES = ["pp_host.cpp", "pp_api.cu", "pp_rope.cu", "pp_attention.cu", "pp_unpack.cu", "pp_unpack_static.cu",
-           "pp_tensorize.cu", "pp_decode.cu"]
+           "pp_tensorize.cu", "pp_decode.cu", "pp_paged.cu", "pp_paged_shared.cu"]
 MODULE_SOURCE = "pp_python.cpp"
-HEADERS = ["pp_internal.h", "pp_device_once.h", "pp_decode_tile.h", "pp_tcgen05.h", os.path.join("..", "..", "include", "pp.h")]
+HEADERS = ["pp_internal.h", "pp_device_once.h", "pp_decode_tile.h", "pp_tcgen05.h", "pp_paged.h", os.path.join("..", "..", "include", "pp.h")]
 
 
 def _nvcc() -> str:

@@ -1,0 +1,95 @@
+// What the translation units of the paged cache share: the cache as the kernels see it, the workspace of the generation
+// step, and the plan of a step in which prompts share pages.
+#ifndef PREPACK_B200_PP_PAGED_H_
+#define PREPACK_B200_PP_PAGED_H_
+
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include <cstddef>
+#include <cstdint>
+
+#include "pp_internal.h"
+
+namespace pp {
+
+constexpr int kMaxPagedPrompts = 8192;   // a step's block sums one number per prompt in shared memory
+constexpr int kSharedTileRows = 256;     // query rows of a work item of the shared rows: two tiles of 128
+constexpr int kSharedTileKeys = 128;
+
+struct PagedCacheArgs {
+  char *k_pages, *v_pages;
+  const float *k_scale, *v_scale;
+  const int32_t* table;
+  int64_t page_stride, head_stride, row_stride;   // bytes
+  int32_t n_pages, page_shift, table_stride;
+};
+inline PagedCacheArgs paged_cache_args(const pp_paged_cache& c) {
+  PagedCacheArgs a;
+  const int64_t size = c.type == PP_CACHE_E4M3 ? 1 : 2;
+  a.k_pages = static_cast<char*>(c.k_pages);
+  a.v_pages = static_cast<char*>(c.v_pages);
+  a.k_scale = c.k_scale;
+  a.v_scale = c.v_scale;
+  a.table = c.page_table;
+  a.page_stride = c.page_stride * size;
+  a.head_stride = c.head_stride * size;
+  a.row_stride = c.row_stride * size;
+  a.n_pages = c.n_pages;
+  a.page_shift = 0;
+  while ((1 << a.page_shift) < c.page_size) ++a.page_shift;
+  a.table_stride = c.table_stride;
+  return a;
+}
+
+struct RopeAngles {
+  double inv_freq[64];                  // theta_j = base^(-2j/D), computed in double on the host
+};
+RopeAngles rope_angles(float base, int32_t head_dim);
+
+// Partial results of a step: (m, l), m in scaled log2 units, and the unnormalised sum of D floats for each (part, query head).
+// Own rows: part = chunk of a prompt. Shared rows (kernel over kSharedTileRows x kSharedTileKeys tiles): the work is a line of
+// units, one tile of keys against one tile of rows each, ordered by (group, KV head, row tile, key tile), and cut into equal
+// pieces, one for each CTA. CTA c's part of an item (group, KV head, row tile) lies at rows c * kSharedTileRows + (rows of all
+// items before it) of the arrays: pieces and items both only ascend, and an item has at most kSharedTileRows rows.
+struct PagedWorkspace {
+  size_t chunk_ptr;                     // int32 [k + 1]
+  size_t part_ml, part_o;               // float2, float[D]
+  // with shared rows only
+  size_t units;                         // int64: units in all
+  size_t unit_start;                    // int64 [n_groups + 1]
+  size_t key_tiles;                     // int32 [n_groups]
+  size_t shared_rows;                   // int32 [n_groups]: rows of pages read for the group
+  size_t lead;                          // int32 [n_groups]: the prompt whose row of the page table stands for the group's
+  size_t own_start;                     // int32 [k]: first row that the prompt reads on its own
+  size_t group_of;                      // int32 [k], -1: none
+  size_t q_rot;                         // bf16 [Hkv][k * group][D]
+  size_t shared_ml, shared_o;           // float2, float[D]
+  size_t total;
+  int32_t chunks_wanted;
+};
+PagedWorkspace paged_workspace(const pp_attn_params& p, int32_t k, int32_t n_groups);
+
+// The plan of the shared rows as the kernels find it in the workspace.
+struct SharedPlan {
+  int64_t* units;
+  int64_t* unit_start;
+  int32_t *key_tiles, *shared_rows, *lead, *own_start, *group_of;
+  __nv_bfloat16* q_rot;
+  float2* ml;
+  float* o;
+  const int32_t* group_ptr;
+  int32_t n_groups, n_ctas;             // n_ctas: pieces that the line of units is cut into
+};
+
+int launch_shared_attention(const pp_attn_params& p, const PagedCacheArgs& c, const SharedPlan& plan, int32_t k, float scale_log2,
+                            int32_t* status, cudaStream_t stream);
+
+#ifdef __CUDACC__
+// Units of each piece.
+__device__ __forceinline__ int64_t units_per_piece(int64_t units, int32_t n_ctas) { return (units + n_ctas - 1) / n_ctas; }
+#endif
+
+}  // namespace pp
+
+#endif  // PREPACK_B200_PP_PAGED_H_

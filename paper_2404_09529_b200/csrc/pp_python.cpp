@@ -23,6 +23,7 @@ class Args {
   ~Args() {
     for (int i = 0; i < n_kept_; ++i) Py_DECREF(kept_[i]);
     if (have_params_) PyBuffer_Release(&params_);
+    if (have_cache_) PyBuffer_Release(&cache_);
   }
   bool count(Py_ssize_t want, const char* name) {
     if (n_ == want) return true;
@@ -42,6 +43,18 @@ class Args {
       return fail<pp_attn_params>();
     }
     return static_cast<const pp_attn_params*>(params_.buf);
+  }
+  // pp_paged_cache from a ctypes structure
+  const pp_paged_cache* cache() {
+    PyObject* x = next();
+    if (failed_) return nullptr;
+    if (PyObject_GetBuffer(x, &cache_, PyBUF_SIMPLE) != 0) return fail<pp_paged_cache>();
+    have_cache_ = true;
+    if (cache_.len < (Py_ssize_t)sizeof(pp_paged_cache)) {
+      PyErr_SetString(PyExc_TypeError, "PagedCache expected");
+      return fail<pp_paged_cache>();
+    }
+    return static_cast<const pp_paged_cache*>(cache_.buf);
   }
   // anything that numpy makes an int32 / int64 array of; `length` receives its first dimension
   const int32_t* i32(Py_ssize_t* length = nullptr) { return static_cast<const int32_t*>(array(NPY_INT32, length)); }
@@ -76,6 +89,13 @@ class Args {
     if (v == -1 && PyErr_Occurred()) failed_ = true;
     return static_cast<int32_t>(v);
   }
+  int64_t integer64() {
+    PyObject* x = next();
+    if (failed_) return 0;
+    const long long v = PyLong_AsLongLong(x);
+    if (v == -1 && PyErr_Occurred()) failed_ = true;
+    return static_cast<int64_t>(v);
+  }
 
  private:
   PyObject* next() { return args_[at_++]; }
@@ -105,8 +125,8 @@ class Args {
   Py_ssize_t n_, at_ = 0;
   PyObject* kept_[8];          // a call has at most seven arrays
   int n_kept_ = 0;
-  bool failed_ = false, have_params_ = false;
-  Py_buffer params_;
+  bool failed_ = false, have_params_ = false, have_cache_ = false;
+  Py_buffer params_, cache_;
 };
 
 #define PP_CALL(expr)            \
@@ -236,6 +256,53 @@ PyObject* decode_step(PyObject*, PyObject* const* args, Py_ssize_t n) {
   PP_CALL(pp_decode_step(p, lengths, static_cast<int32_t>(k), q, kn, vn, o, kc, vc, off, cap, ws, host, bytes, stream));
 }
 
+// paged_append(params, cache, prompt, position, n_rows, n_prompts, k_new, k_stride, v_new, v_stride, device_status, stream)
+PyObject* paged_append(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  Args a(args, n);
+  if (!a.count(12, "paged_append")) return nullptr;
+  const pp_attn_params* p = a.params();
+  const pp_paged_cache* c = a.cache();
+  void *prompt = a.address(), *position = a.address();
+  const int64_t n_rows = a.integer64();
+  const int32_t n_prompts = a.integer();
+  void* k = a.address();
+  const int64_t k_stride = a.integer64();
+  void* v = a.address();
+  const int64_t v_stride = a.integer64();
+  void *st = a.address(), *stream = a.address();
+  if (a.failed()) return nullptr;
+  PP_CALL(pp_paged_append(p, c, static_cast<const int32_t*>(prompt), static_cast<const int32_t*>(position), n_rows, n_prompts, k, k_stride, v,
+                          v_stride, static_cast<int32_t*>(st), stream));
+}
+
+// paged_decode(params, cache, lengths, k, group_ptr, shared_len, n_groups, q_new, q_stride, k_new, k_stride, v_new, v_stride, o, workspace,
+//              workspace_bytes, device_status, stream); n_groups < 0: pp_paged_decode_step, else pp_paged_decode_shared
+PyObject* paged_decode(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  Args a(args, n);
+  if (!a.count(18, "paged_decode")) return nullptr;
+  const pp_attn_params* p = a.params();
+  const pp_paged_cache* c = a.cache();
+  const int32_t* lengths = static_cast<const int32_t*>(a.address());
+  const int32_t k = a.integer();
+  const int32_t *ptr = static_cast<const int32_t*>(a.address()), *shared = static_cast<const int32_t*>(a.address());
+  const int32_t n_groups = a.integer();
+  void* q = a.address();
+  const int64_t q_stride = a.integer64();
+  void* kn = a.address();
+  const int64_t k_stride = a.integer64();
+  void* vn = a.address();
+  const int64_t v_stride = a.integer64();
+  void *o = a.address(), *ws = a.address();
+  const size_t bytes = a.size();
+  int32_t* st = static_cast<int32_t*>(a.address());
+  void* stream = a.address();
+  if (a.failed()) return nullptr;
+  if (n_groups < 0) {
+    PP_CALL(pp_paged_decode_step(p, c, lengths, k, q, q_stride, kn, k_stride, vn, v_stride, o, ws, bytes, st, stream));
+  }
+  PP_CALL(pp_paged_decode_shared(p, c, lengths, k, ptr, shared, n_groups, q, q_stride, kn, k_stride, vn, v_stride, o, ws, bytes, st, stream));
+}
+
 // ------------------------------------------------------------------------------------------
 // Fence: a CUDA event without timing, made on its first record (on the device that is current then).
 // ------------------------------------------------------------------------------------------
@@ -289,7 +356,8 @@ PyType_Spec fence_spec = {"paper_2404_09529_b200._native.Fence", sizeof(Fence), 
 
 #define PP_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {PP_METHOD(pack), PP_METHOD(prefill_fused), PP_METHOD(prefill_attention), PP_METHOD(unpack_kv),
-                         PP_METHOD(decode_workspace_bytes), PP_METHOD(decode_step), {nullptr, nullptr, 0, nullptr}};
+                         PP_METHOD(decode_workspace_bytes), PP_METHOD(decode_step),
+                         PP_METHOD(paged_append), PP_METHOD(paged_decode), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

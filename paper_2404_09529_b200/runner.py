@@ -250,3 +250,225 @@ class DecodeBatch:
         self._copied[slot].record(stream)
         self.lengths += 1
         return self.o
+
+
+class PagedCaches:
+    """KV caches in pages: two pools of pages and the table that says which pages every prompt has (see
+    ``pp_paged_cache`` in include/pp.h). The tensors may come from the caller, who then keeps the table; `allocate` makes
+    them, and `reserve`, `share` and `release` hand pages out. Memory plumbing only."""
+
+    TYPES = {torch.bfloat16: B.PP_CACHE_BF16, torch.float8_e4m3fn: B.PP_CACHE_E4M3}
+
+    def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.Tensor, rows_first: bool = False,
+                 k_scale: torch.Tensor | None = None, v_scale: torch.Tensor | None = None):
+        """k_pages, v_pages: [n_pages, Hkv, page_size, D], or with rows_first [n_pages, page_size, Hkv, D]; bf16, or float8_e4m3fn
+        with k_scale and v_scale (float32 [Hkv]). page_table: int32 [prompts, most pages of a prompt]."""
+        head, row = (2, 1) if rows_first else (1, 2)
+        if k_pages.dtype not in self.TYPES or k_pages.dim() != 4 or k_pages.stride(3) != 1:
+            raise ValueError("pages are 4-D bfloat16 or float8_e4m3fn tensors, contiguous in the last dimension")
+        if (v_pages.shape, v_pages.stride(), v_pages.dtype, v_pages.device) != (k_pages.shape, k_pages.stride(), k_pages.dtype, k_pages.device):
+            raise ValueError("both pools have one shape, layout, type and device")
+        if page_table.dtype != torch.int32 or page_table.dim() != 2 or page_table.device != k_pages.device or not page_table.is_contiguous():
+            raise ValueError("the page table is a contiguous 2-D int32 tensor on the pools' device")
+        self.n_pages, self.page_size = k_pages.shape[0], k_pages.shape[row]
+        self.hkv, self.d = k_pages.shape[head], k_pages.shape[3]
+        self.n_prompts = page_table.shape[0]
+        e4m3 = k_pages.dtype == torch.float8_e4m3fn
+        for scale in (k_scale, v_scale):
+            if (scale is not None) != e4m3:
+                raise ValueError("8-bit pages, and only they, have scales")
+            if e4m3 and (scale.dtype != torch.float32 or scale.shape != (self.hkv,) or scale.device != k_pages.device or not scale.is_contiguous()):
+                raise ValueError("a scale is a contiguous float32 [Hkv] tensor on the pools' device")
+        self.device, self.rows_first = k_pages.device, rows_first
+        self.k_pages, self.v_pages, self.page_table, self.k_scale, self.v_scale = k_pages, v_pages, page_table, k_scale, v_scale
+        self.struct = B.PagedCache(
+            k_pages.data_ptr(), v_pages.data_ptr(), k_scale.data_ptr() if e4m3 else None, v_scale.data_ptr() if e4m3 else None,
+            page_table.data_ptr(), k_pages.stride(0), k_pages.stride(head), k_pages.stride(row), self.n_pages, self.page_size,
+            page_table.shape[1], self.TYPES[k_pages.dtype])
+        self.status = torch.zeros(1, dtype=torch.int32, device=self.device)
+        self._append_params = {}
+        self._count = self._users = None
+
+    @classmethod
+    def allocate(cls, n_prompts: int, n_pages: int, max_rows: int, n_kv_heads: int, head_dim: int, page_size: int = 64,
+                 dtype: torch.dtype = torch.bfloat16, rows_first: bool = False, device: str = "cuda",
+                 k_scale: torch.Tensor | None = None, v_scale: torch.Tensor | None = None) -> "PagedCaches":
+        """Pools of n_pages zeroed pages and an empty table for n_prompts prompts of up to max_rows rows."""
+        shape = (n_pages, page_size, n_kv_heads, head_dim) if rows_first else (n_pages, n_kv_heads, page_size, head_dim)
+        pools = [torch.zeros(shape, dtype=torch.bfloat16, device=device).to(dtype) for _ in range(2)]
+        table = torch.full((n_prompts, -(-max_rows // page_size)), -1, dtype=torch.int32, device=device)
+        self = cls(*pools, table, rows_first, k_scale, v_scale)
+        self._table = np.full(tuple(table.shape), -1, dtype=np.int32)     # what the device table holds
+        self._count = np.zeros(n_prompts, dtype=np.int64)                 # pages that each prompt has
+        self._users = np.zeros(n_pages, dtype=np.int64)                   # prompts that have each page
+        self._free = list(range(n_pages - 1, -1, -1))
+        return self
+
+    def _owned(self) -> None:
+        if self._count is None:
+            raise ValueError("the table of these caches belongs to the caller")
+
+    def _write_row(self, prompt: int) -> None:
+        self.page_table[prompt].copy_(torch.from_numpy(self._table[prompt].copy()))
+
+    def reserve(self, prompt: int, rows: int) -> None:
+        """Pages for rows 0 .. rows - 1 of a prompt, in addition to those it has."""
+        self._owned()
+        have, want = int(self._count[prompt]), -(-rows // self.page_size)
+        if want > self._table.shape[1]:
+            raise ValueError(f"{rows} rows do not fit the prompt's row of the page table")
+        if want <= have:
+            return
+        if want - have > len(self._free):
+            raise MemoryError(f"{want - have} pages wanted, {len(self._free)} free")
+        pages = [self._free.pop() for _ in range(want - have)]
+        self._table[prompt, have:want] = pages
+        self._users[pages] = 1
+        self._count[prompt] = want
+        self._write_row(prompt)
+
+    def share(self, source: int, prompt: int, rows: int) -> int:
+        """Gives an empty prompt the pages of `source` that lie wholly within its first `rows` rows. Returns how many rows those
+        are; the rows behind them are the prompt's own (append them again)."""
+        self._owned()
+        n = rows // self.page_size
+        if self._count[prompt]:
+            raise ValueError("the prompt has pages already")
+        if n > self._count[source]:
+            raise ValueError("the source does not have that many rows")
+        self._table[prompt, :n] = self._table[source, :n]
+        self._users[self._table[source, :n]] += 1
+        self._count[prompt] = n
+        self._write_row(prompt)
+        return n * self.page_size
+
+    def release(self, prompt: int) -> None:
+        """Gives a prompt's pages back, those at least that no other prompt has."""
+        self._owned()
+        pages = self._table[prompt, :self._count[prompt]]
+        self._users[pages] -= 1
+        self._free.extend(int(p) for p in pages if self._users[p] == 0)
+        self._table[prompt] = -1
+        self._count[prompt] = 0
+        self._write_row(prompt)
+
+    def check_new(self, x: torch.Tensor, rows: int, heads: int, what: str) -> int:
+        """The row stride of new rows [rows, heads, D]; slices of a fused projection are welcome."""
+        if x.dtype != torch.bfloat16 or x.device != self.device or tuple(x.shape) != (rows, heads, self.d):
+            raise ValueError(f"{what}: a bfloat16 tensor of shape {(rows, heads, self.d)} on {self.device} is wanted")
+        if x.stride(2) != 1 or (heads > 1 and x.stride(1) != self.d):
+            raise ValueError(f"{what}: the heads of a row lie one behind the other")
+        if rows > 1 and x.stride(0) < heads * self.d:
+            raise ValueError(f"{what}: every row has memory of its own")
+        return x.stride(0) if rows > 1 else 0
+
+    def append(self, prompt: torch.Tensor, position: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, rope_base: float,
+               rotated: bool = False) -> None:
+        """Row r of k_new, v_new [rows, Hkv, D] becomes row position[r] of prompt[r] (int32 tensors on the device; prompt < 0: no
+        row), its key rotated by that position unless it is rotated already. On the current stream, asynchronous."""
+        rows = prompt.shape[0]
+        for x in (prompt, position):
+            if x.dtype != torch.int32 or x.shape != (rows,) or x.device != self.device or not x.is_contiguous():
+                raise ValueError("prompt and position are contiguous int32 tensors of one length on the pools' device")
+        strides = [self.check_new(x, rows, self.hkv, what) for x, what in ((k_new, "k_new"), (v_new, "v_new"))]
+        key = (rope_base, rotated)
+        params = self._append_params.get(key)
+        if params is None:
+            params = B.AttnParams(self.hkv, self.hkv, self.d, rope_base, 0.0, 1, 1, B.PP_FLAG_SKIP_ROPE if rotated else 0)
+            self._append_params[key] = params
+        with on_device(self.device):
+            B.pp_paged_append(params, self.struct, prompt, position, rows, self.n_prompts, k_new, strides[0], v_new, strides[1],
+                              self.status, B.current_stream())
+
+    def append_prefill(self, prefill: PrefillBatch) -> torch.Tensor:
+        """UNPACK into pages: the rotated keys and the values of a PrefillBatch that has run, prompt i of the batch into
+        prompt i here (`reserve` its rows first). Returns the lengths, int32 on the device."""
+        segment = np.full((prefill.pack.n_bins, prefill.pack.capacity), -1, dtype=np.int32)
+        position = np.zeros_like(segment)
+        for i, n in enumerate(prefill.lengths):
+            at = slice(int(prefill.off_of[i]), int(prefill.off_of[i]) + int(n))
+            segment[prefill.bin_of[i], at] = i
+            position[prefill.bin_of[i], at] = np.arange(n)
+        segment, position = (torch.from_numpy(x.reshape(-1)).to(self.device) for x in (segment, position))
+        rows = segment.shape[0]
+        self.append(segment, position, prefill.kk.view(rows, self.hkv, self.d), prefill.v.view(rows, self.hkv, self.d),
+                    prefill.rope_base, rotated=True)
+        return torch.from_numpy(prefill.lengths).to(self.device)
+
+
+class _Nothing:
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *_):
+        return False
+
+
+_NOTHING = _Nothing()
+
+
+def on_device(device: torch.device):
+    """Makes `device` the current one, where it is not (the C ABI launches on the current device)."""
+    return _NOTHING if torch._C._cuda_getDevice() == device.index else torch.cuda.device(device)
+
+
+class PagedDecoder:
+    """Generation steps over PagedCaches through pp_paged_decode_step / pp_paged_decode_shared. Owns the workspace (of the steps
+    of one stream: steps that may run at the same time want a decoder each) and the status word."""
+
+    def __init__(self, caches: PagedCaches, n_q_heads: int, rope_base: float, softmax_scale: float = 0.0):
+        self.caches, self.hq = caches, n_q_heads
+        self.params = B.AttnParams(n_q_heads, caches.hkv, caches.d, rope_base, softmax_scale, 1, 1, 0)
+        self.status = torch.zeros(1, dtype=torch.int32, device=caches.device)
+        # Workspaces are kept when a larger one is wanted: a captured graph may go on using them.
+        self._workspaces = []
+        self._sizes = {}
+
+    def _workspace(self, k: int, n_groups: int) -> torch.Tensor:
+        need = self._sizes.get((k, n_groups))
+        if need is None:
+            need = B.pp_paged_decode_workspace_bytes(self.params, k, n_groups)
+            if need == 0:
+                raise ValueError("no generation step for these shapes")
+            self._sizes[(k, n_groups)] = need
+        if not self._workspaces or self._workspaces[-1].numel() < need:
+            self._workspaces.append(torch.empty(need, dtype=torch.uint8, device=self.caches.device))
+        return self._workspaces[-1]
+
+    def step(self, lengths: torch.Tensor, q: torch.Tensor, k: torch.Tensor | None = None, v: torch.Tensor | None = None,
+             out: torch.Tensor | None = None, groups=None) -> torch.Tensor:
+        """One token for each prompt of the table's first len(lengths) rows. lengths: int32 on the device, rows that the pages hold
+        (< 0: no prompt). q [n, Hq, D]; k, v [n, Hkv, D]: the new token, appended; or None: the pages hold it. groups: (group_ptr,
+        shared_len), int32 on the device, where prompts share their first pages. Returns out [n, Hq, D]; on the
+        current stream, asynchronous, nothing is read back. The lengths are the caller's to advance."""
+        c = self.caches
+        n = lengths.shape[0]
+        if lengths.dtype != torch.int32 or lengths.dim() != 1 or lengths.device != c.device or not lengths.is_contiguous() or not 0 < n <= c.n_prompts:
+            raise ValueError("lengths: a contiguous int32 tensor on the pools' device, of at most the table's rows")
+        if (k is None) != (v is None):
+            raise ValueError("a new token has a key and a value")
+        q_stride = c.check_new(q, n, self.hq, "q")
+        k_stride, v_stride = (0, 0) if k is None else (c.check_new(k, n, c.hkv, "k"), c.check_new(v, n, c.hkv, "v"))
+        if out is None:
+            out = torch.zeros((n, self.hq, c.d), dtype=torch.bfloat16, device=c.device)
+        elif out.dtype != torch.bfloat16 or tuple(out.shape) != (n, self.hq, c.d) or out.device != c.device or not out.is_contiguous():
+            raise ValueError("out: a contiguous bfloat16 tensor of q's shape on the pools' device")
+        with on_device(c.device):
+            if groups is None:
+                ws = self._workspace(n, 0)
+                B.pp_paged_decode_step(self.params, c.struct, lengths, n, q, q_stride, k, k_stride, v, v_stride, out, ws, ws.numel(),
+                                       self.status, B.current_stream())
+            else:
+                ptr, shared = groups
+                for x in (ptr, shared):
+                    if x.dtype != torch.int32 or x.dim() != 1 or x.device != c.device or not x.is_contiguous():
+                        raise ValueError("groups: contiguous int32 tensors on the pools' device")
+                if ptr.shape[0] != shared.shape[0] + 1:
+                    raise ValueError("groups: group_ptr has one entry more than shared_len")
+                ws = self._workspace(n, shared.shape[0])
+                B.pp_paged_decode_shared(self.params, c.struct, lengths, n, ptr, shared, shared.shape[0], q, q_stride, k, k_stride, v,
+                                         v_stride, out, ws, ws.numel(), self.status, B.current_stream())
+        return out
+
+    def device_status(self) -> int:
+        return int(self.status.item())
