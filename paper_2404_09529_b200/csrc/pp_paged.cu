@@ -12,6 +12,7 @@
 #include "pp_decode_tile.h"
 #include "pp_device_once.h"
 #include "pp_paged.h"
+#include "pp_tcgen05.h"
 
 namespace pp {
 namespace {
@@ -28,6 +29,16 @@ __device__ __forceinline__ void angle(int position, double inv_freq, float& cs, 
   double red = fma(-n, 6.283185307179586, ang);
   red = fma(-n, 2.4492935982947064e-16, red);
   sincosf((float)red, &sn, &cs);
+}
+// Those of four neighbouring elements, one after another: the code of a sine is long, and instructions have to be fetched too.
+__device__ __forceinline__ void angles4(int position, const double* inv_freq, float (&cs)[4], float (&sn)[4]) {
+#pragma unroll 1
+  for (int e = 0; e < 4; ++e) {
+    float c, s;
+    angle(position, inv_freq[e], c, s);
+    cs[0] = cs[1]; cs[1] = cs[2]; cs[2] = cs[3]; cs[3] = c;
+    sn[0] = sn[1]; sn[1] = sn[2]; sn[2] = sn[3]; sn[3] = s;
+  }
 }
 __device__ __forceinline__ float turn_lo(float a, float b, float cs, float sn) { return __fmaf_rn(a, cs, -__fmul_rn(b, sn)); }
 __device__ __forceinline__ float turn_hi(float a, float b, float cs, float sn) { return __fmaf_rn(b, cs, __fmul_rn(a, sn)); }
@@ -193,17 +204,27 @@ append_kernel(const __grid_constant__ AppendArgs a) {
 // ------------------------------------------------------------------------------------------
 // One generation step
 // ------------------------------------------------------------------------------------------
-// Work: a prompt's rows are cut into chunks of equal size, a whole number of 64-row blocks, such that all prompts together
-// make about kChunksWanted (chunk, KV head) pieces; persistent CTAs take them in turn. The lengths live on the device, so every
-// CTA sums them itself (one or two loads per thread, two passes of the block), and the grid and the room for partial results
-// depend on k and the heads alone: sum of ceil(blocks_i / C) <= kChunksWanted / Hkv + k with C the block count that
-// divides all blocks into kChunksWanted / Hkv.
-constexpr int kPagedThreads = 128;
-constexpr int kPagedWarps = kPagedThreads / 32;
+// Bound: HBM, every row of K and V is read once. The work is a line of units of 8 KB (16, 32 or 64 rows of K and V of one KV
+// head), ordered by (prompt, KV head, rows), and cut into equal pieces, one for each warp that the GPU holds: all warps read the
+// same number of bytes whatever the lengths are. A warp works on its own from there on. Its rows arrive by TMA in a ring of
+// two units in shared memory, whose loads run ahead over the ends of items, so that 12 warps keep up to 192 KB of an SM under
+// way. A piece that is a whole item (prompt, KV head) leaves O at once; of an item that is cut the parts (m, l, o) are joined by
+// paged_combine_kernel.
+// The arithmetic is that of the step over contiguous caches (pp_decode.cu): mma.m16n8k16 with 16 keys as rows and the query heads
+// of a KV head as the 8 columns, absent heads 0. A query and a weight each reach it as the sum of two 16-bit numbers: HBM
+// leaves the tensor cores idle, and scores and O are then exact to 2^-16, far below O's last rounding of 2^-8.
+// The lengths live on the device: every CTA sums them itself, and the grid and the room for parts depend on neither them nor k.
 constexpr int kMaxGroup = 8;            // query heads per KV head: the N of the tensor-core product
-constexpr int kStepKeys = 16;           // keys per warp and step
-constexpr int kBlockKeys = kStepKeys * kPagedWarps;
-constexpr int kChunksWanted = kSms * 3 * 4;
+constexpr int kStepWarps = 12, kStepThreads = 32 * kStepWarps;
+constexpr int kPieces = kSms * kStepWarps;
+constexpr int kHalfUnit = 4096;         // bytes of K, and of V, in a unit
+constexpr int kScratch = 2304;          // per warp: queries, the new token's rows, O on its way out
+constexpr int kStepSmem = 1024 + kStepWarps * (4 * kHalfUnit + kScratch);    // rings on 1024-byte boundaries
+constexpr int kCombineThreads = 256, kCombineBlocks = 4 * kSms;
+// The running maximum of a row moves only when a score exceeds it by more than 2^kLazyLog2: until then no lane has to ask the
+// others (three exchanges for each of two heads). Sums are at most 2^kLazyLog2 as large, which costs fp32 nothing.
+constexpr float kLazyLog2 = 4.f;
+enum WaitCode { kWaitRows = 41 };
 
 struct PagedArgs {
   PagedCacheArgs c;
@@ -212,12 +233,13 @@ struct PagedArgs {
   const __nv_bfloat16 *q_new, *k_new, *v_new;
   int64_t q_stride, k_stride, v_stride;
   __nv_bfloat16* o;
-  int32_t* chunk_ptr;                   // [k + 1], left by CTA 0 for the kernel that joins the chunks
-  float2* part_ml;                      // [chunk][Hq]
-  float* part_o;                        // [chunk][Hq][D]
-  int32_t n_prompts, n_q_heads, n_kv_heads, group, chunks_wanted;
+  int4* cut;                            // [kPieces]: of the item that begins in a piece and ends in another: prompt, KV head, pieces; 0 pieces: none
+  float2* part_ml;                      // [2 kPieces][group]
+  float* part_o;                        // [2 kPieces][group][D]
+  int32_t n_prompts, n_q_heads, n_kv_heads, group;
   float scale_log2;
   int32_t* status;
+  uint32_t wait_limit;                  // in units of 1024 ns
   RopeAngles angles;
 };
 
@@ -232,22 +254,9 @@ __device__ __forceinline__ int checked_length(const PagedCacheArgs& c, const int
   return max(len, -1);
 }
 
-// Sum over the block's threads; every thread gets it. (Two barriers.)
+// Exclusive prefix sum over the block's threads, and the sum of all. (Two barriers.)
 template <int kThreads>
-__device__ __forceinline__ int64_t block_sum(int64_t x, int64_t* s_warp) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-  if ((threadIdx.x & 31) == 0) s_warp[threadIdx.x >> 5] = x;
-  __syncthreads();
-  int64_t sum = 0;
-#pragma unroll
-  for (int w = 0; w < kThreads / 32; ++w) sum += s_warp[w];
-  __syncthreads();
-  return sum;
-}
-// Exclusive prefix sum over the block's threads.
-template <int kThreads>
-__device__ __forceinline__ int64_t block_prefix(int64_t x, int64_t* s_warp) {
+__device__ __forceinline__ int64_t block_prefix(int64_t x, int64_t* s_warp, int64_t& total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   int64_t sum = x;
 #pragma unroll
@@ -258,53 +267,41 @@ __device__ __forceinline__ int64_t block_prefix(int64_t x, int64_t* s_warp) {
   if (lane == 31) s_warp[warp] = sum;
   __syncthreads();
   int64_t before = 0;
+  total = 0;
 #pragma unroll
-  for (int w = 0; w < kThreads / 32; ++w)
+  for (int w = 0; w < kThreads / 32; ++w) {
     if (w < warp) before += s_warp[w];
+    total += s_warp[w];
+  }
   __syncthreads();
   return before + sum - x;
 }
 
-// Blocks per chunk; s_ptr[0 .. k]: first chunk of every prompt. A prompt without rows of its own has one chunk all the same, in
-// which its output is written; a row of no prompt has none.
-__device__ __forceinline__ int cut_into_chunks(const PagedArgs& a, int32_t* s_ptr, int64_t* s_warp) {
-  const int k = a.n_prompts, tid = threadIdx.x;
-  const bool fresh = a.k_new != nullptr;
-  const int each = (k + kPagedThreads - 1) / kPagedThreads, i0 = min(tid * each, k), i1 = min(i0 + each, k);
-  int32_t* status = blockIdx.x == 0 ? a.status : nullptr;
-  int64_t blocks = 0;
-  for (int i = i0; i < i1; ++i) {
-    const int len = checked_length(a.c, a.lengths, i, fresh, status);
-    const int n = len < 0 ? -1 : (len - (a.own_start ? a.own_start[i] : 0) + kBlockKeys - 1) / kBlockKeys;
-    s_ptr[i] = n;
-    blocks += max(n, 0);
-  }
-  const int64_t total = block_sum<kPagedThreads>(blocks, s_warp);
-  const int chunk_blocks = (int)max((total + a.chunks_wanted - 1) / a.chunks_wanted, (int64_t)1);
-  int64_t mine = 0;
-  for (int i = i0; i < i1; ++i) {
-    const int n = s_ptr[i];
-    const int chunks = n < 0 ? 0 : max((n + chunk_blocks - 1) / chunk_blocks, 1);
-    s_ptr[i] = chunks;
-    mine += chunks;
-  }
-  int at = (int)block_prefix<kPagedThreads>(mine, s_warp);
-  for (int i = i0; i < i1; ++i) {
-    const int chunks = s_ptr[i];
-    s_ptr[i] = at;
-    at += chunks;
-  }
-  if (tid == kPagedThreads - 1) s_ptr[k] = at;
-  __syncthreads();
-  return chunk_blocks;
+// A box of a page: 16 rows of one head. Coordinates: column (0), row of the page, chunk of 64 columns (0: all of them), head, page.
+// Every lane whose `issue` is set loads its own; beyond the last page: zeros.
+__device__ __forceinline__ void load_rows(uint32_t dst, const CUtensorMap* map, uint32_t bar, int row, int head, int page, uint32_t issue) {
+  asm volatile(
+      "{\n.reg .pred q;\nsetp.ne.b32 q, %6, 0;\n"
+      "@q cp.async.bulk.tensor.5d.shared::cluster.global.mbarrier::complete_tx::bytes"
+      " [%0], [%1, {%7, %3, %7, %4, %5}], [%2];\n}"
+      ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(row), "r"(head), "r"(page), "r"(issue), "r"(0) : "memory");
 }
-
-// 16 keys of a warp in e4m3: K rows g and g + 8, 16-byte pieces t, t + 4 of a row (D = 64: piece t); V rows 2t, 2t + 1, 2t + 8,
-// 2t + 9, the g-th eighth of a row. The numbers are multiplied as f16, which holds every e4m3 number.
-template <int D>
-struct StepK8 { uint4 r[2][D / 64]; };
-template <int D>
-struct StepV8 { uint32_t r[4][D / 32]; };
+__device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void ldmatrix4_trans(uint32_t (&r)[4], uint32_t at) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ uint4 shared16(uint32_t at) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint2 shared8(uint32_t at) {
+  uint2 v;
+  asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at) : "memory");
+  return v;
+}
 
 __device__ __forceinline__ void mma16816_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -322,66 +319,116 @@ __device__ __forceinline__ uint32_t f16_of_e4m3_hi(uint32_t x) {
   return y;
 }
 
-// What differs between pages of bf16 and of e4m3: how a step's rows are loaded and multiplied.
+// What differs between pages of bf16 and of e4m3: where a row's 16-byte pieces stand in shared memory, and how 16 keys are
+// multiplied. Lane = 4 g + t. A: 16 keys (g, g + 8) by 16 elements, or 16 elements of O (`element`) by 16 keys. q: D / 8 words of a
+// thread for the upper part of the queries, as many for the lower one.
 template <int D, bool kE4m3>
 struct Rows;
 
 template <int D>
 struct Rows<D, false> {
-  using K = StepK<D>;
-  using V = StepV<D>;
-  // Row pitch of the queries in shared memory, in 16-bit elements: rows 64 bytes apart modulo 128 serve the 8 lanes of a
-  // 16-byte access without conflicts
-  static constexpr int kPitch = D + 32;
-  static constexpr int kQ = D / 32;                   // 16-byte pieces of a query that a thread meets
+  static constexpr int kRowBytes = 2 * D, kSteps = kHalfUnit / (16 * kRowBytes);      // steps of 16 keys in a unit
   static constexpr float kWeight = 1.f;
-  static __device__ __forceinline__ void load_k(K& f, const char* p, int64_t row_stride, int g, int t) {
+  // A step's box, as TMA leaves it: chunks of 64 elements one behind the other, rows of 128 bytes, the 16-byte pieces of 8 rows
+  // swizzled so that one of each row fill all banks once.
+  static constexpr int kStepBytes = 16 * kRowBytes, kChunkBytes = 2048;
+  static __device__ __forceinline__ int row_of(int at) { return (D == 128 ? 0 : (at >> 11) * 16) + ((at >> 7) & 15); }   // of byte `at` of a unit
+  static __device__ __forceinline__ void load_q(uint32_t (&q)[D / 8], uint32_t row_at, int t) {
 #pragma unroll
-    for (int x = 0; x < 2; ++x)
+    for (int kk = 0; kk < D / 16; ++kk)
 #pragma unroll
-      for (int i = 0; i < D / 32; ++i)
-        f.r[x][i] = load16(reinterpret_cast<const __nv_bfloat16*>(p + (g + 8 * x) * row_stride) + 8 * t + 32 * i);
+      for (int x = 0; x < 2; ++x)
+        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(q[2 * kk + x]) : "r"(row_at + 32 * kk + 16 * x + 4 * t) : "memory");
   }
-  static __device__ __forceinline__ void load_v(V& f, const char* p, int64_t row_stride, int g, int t) {
+  static __device__ __forceinline__ void mma_scores(float (&c)[4], const uint32_t (*a)[4], const uint32_t (&qh)[D / 8], const uint32_t (&ql)[D / 8]) {
+    // four chains of products instead of one: each waits for the one before it
+    float p[4][4];
 #pragma unroll
-    for (int x = 0; x < 4; ++x)
+    for (int x = 0; x < 4; ++x) p[x][0] = p[x][1] = p[x][2] = p[x][3] = 0.f;
 #pragma unroll
-      for (int i = 0; i < D / 64; ++i)
-        f.r[x][i] = load16(reinterpret_cast<const __nv_bfloat16*>(p + (2 * t + (x & 1) + 8 * (x >> 1)) * row_stride) + 8 * g + 64 * i);
-  }
-  // the new token's rows, from shared memory, as a step with one real key
-  static __device__ __forceinline__ void one_row(K& fk, V& fv, const uint8_t* k_row, const uint8_t* v_row, int g, int t) {
-    const uint4 none = make_uint4(0u, 0u, 0u, 0u);
-#pragma unroll
-    for (int i = 0; i < D / 32; ++i) {
-      fk.r[0][i] = g == 0 ? *reinterpret_cast<const uint4*>(k_row + 16 * t + 64 * i) : none;
-      fk.r[1][i] = none;
+    for (int kk = 0; kk < D / 16; ++kk) {
+      mma16816(p[kk & 1], a[kk][0], a[kk][1], a[kk][2], a[kk][3], qh[2 * kk], qh[2 * kk + 1]);
+      mma16816(p[2 + (kk & 1)], a[kk][0], a[kk][1], a[kk][2], a[kk][3], ql[2 * kk], ql[2 * kk + 1]);
     }
 #pragma unroll
-    for (int x = 0; x < 4; ++x)
-#pragma unroll
-      for (int i = 0; i < D / 64; ++i) fv.r[x][i] = x == 0 && t == 0 ? *reinterpret_cast<const uint4*>(v_row + 16 * g + 128 * i) : none;
+    for (int x = 0; x < 4; ++x) c[x] = (p[0][x] + p[1][x]) + (p[2][x] + p[3][x]);
   }
-  // piece i of query `row` that this thread's K pieces meet
-  static __device__ __forceinline__ uint4 q_piece(const uint16_t* q, int t, int i) { return *reinterpret_cast<const uint4*>(q + 8 * t + 32 * i); }
-  static __device__ __forceinline__ void scores(float (&c)[4], const K& f, const uint4 (&q)[kQ], const uint16_t* q_low, int t) {
-    c[0] = c[1] = c[2] = c[3] = 0.f;
+  // scores of the 16 rows that begin at `at`
+  static __device__ __forceinline__ void scores(float (&c)[4], uint32_t at, const uint32_t (&qh)[D / 8], const uint32_t (&ql)[D / 8], int lane) {
+    uint32_t a[D / 16][4];
+    const uint32_t from = at + ((lane & 7) + (lane & 8)) * 128 + (((lane >> 4) ^ (lane & 7)) << 4);
 #pragma unroll
-    for (int i = 0; i < kQ; ++i) {
-      const uint4 l = q_piece(q_low, t, i);
-      mma16816(c, f.r[0][i].x, f.r[1][i].x, f.r[0][i].y, f.r[1][i].y, l.x, l.y);
-      mma16816(c, f.r[0][i].z, f.r[1][i].z, f.r[0][i].w, f.r[1][i].w, l.z, l.w);
+    for (int kk = 0; kk < D / 16; ++kk) ldmatrix4(a[kk], (from ^ ((kk & 3) << 5)) + (kk >> 2) * kChunkBytes);
+    mma_scores(c, a, qh, ql);
+  }
+  // a row of its own, as the first of 16
+  static __device__ __forceinline__ void scores_one(float (&c)[4], uint32_t at, const uint32_t (&qh)[D / 8], const uint32_t (&ql)[D / 8], int g, int t) {
+    uint32_t a[D / 16][4];
+#pragma unroll
+    for (int kk = 0; kk < D / 16; ++kk) {
+      uint32_t x, y;
+      asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x) : "r"(at + 32 * kk + 4 * t) : "memory");
+      asm volatile("ld.shared.u32 %0, [%1];" : "=r"(y) : "r"(at + 32 * kk + 16 + 4 * t) : "memory");
+      a[kk][0] = g == 0 ? x : 0u;
+      a[kk][1] = 0u;
+      a[kk][2] = g == 0 ? y : 0u;
+      a[kk][3] = 0u;
     }
+    mma_scores(c, a, qh, ql);
+  }
+  // P in two parts of 8 bits, the first cut and not rounded, so that neither is negative, and none of a weight above 0 (which is
+  // at least 2^-126) is 0: an infinite value then gives an infinity and not a NaN, a finite one up to 2^-125 of itself too much.
+  struct Weights { uint32_t b[2][2]; };
+  static __device__ __forceinline__ Weights weights(const float (&p)[4]) {
+    Weights w;
 #pragma unroll
-    for (int i = 0; i < kQ; ++i) {
-      mma16816(c, f.r[0][i].x, f.r[1][i].x, f.r[0][i].y, f.r[1][i].y, q[i].x, q[i].y);
-      mma16816(c, f.r[0][i].z, f.r[1][i].z, f.r[0][i].w, f.r[1][i].w, q[i].z, q[i].w);
+    for (int x = 0; x < 2; ++x) {
+      const float p0 = p[2 * x], p1 = p[2 * x + 1];
+      const uint32_t cut = truncate_bf16x2(p0, p1), least = (p0 > 0.f ? 0x0080u : 0u) | (p1 > 0.f ? 0x00800000u : 0u);
+      const float2 back = unpack_bf16(cut);
+      const uint32_t rest = round_bf16(p0 - back.x, p1 - back.y);
+      const __nv_bfloat162 low = __hmax2_nan(*reinterpret_cast<const __nv_bfloat162*>(&rest), *reinterpret_cast<const __nv_bfloat162*>(&least));
+      w.b[0][x] = transpose8x8(cut);
+      w.b[1][x] = transpose8x8(*reinterpret_cast<const uint32_t*>(&low));
+    }
+    return w;
+  }
+  static __device__ __forceinline__ void add(float (&acc)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, const Weights& w) {
+    mma16816(acc, a0, a1, a2, a3, w.b[1][0], w.b[1][1]);
+    mma16816(acc, a0, a1, a2, a3, w.b[0][0], w.b[0][1]);
+  }
+  static __device__ __forceinline__ void product(float (&acc)[D / 16][4], uint32_t at, const float (&p)[4], int lane) {
+    const Weights w = weights(p);
+    const uint32_t from = at + ((lane & 7) + ((lane >> 1) & 8)) * 128 + ((((lane >> 3) & 1) ^ (lane & 7)) << 4);
+#pragma unroll
+    for (int j = 0; j < D / 16; ++j) {
+      uint32_t a[4];
+      ldmatrix4_trans(a, (from ^ ((j & 3) << 5)) + (j >> 2) * kChunkBytes);
+      add(acc[j], a[0], a[1], a[2], a[3], w);
     }
   }
-  static __device__ __forceinline__ void clear(V& f, int n_real, int t) { clear_past<D>(f, n_real, t); }
-  static __device__ __forceinline__ void product(Softmax<D>& s, const V& f, const float (&p)[4]) { pv<D>(s, f, p); }
+  static __device__ __forceinline__ void product_one(float (&acc)[D / 16][4], uint32_t at, const float (&p)[4], int g, int t) {
+    const Weights w = weights(p);
+#pragma unroll
+    for (int j = 0; j < D / 16; ++j) {
+      uint16_t x, y;
+      asm volatile("ld.shared.u16 %0, [%1];" : "=h"(x) : "r"(at + 2 * (16 * j + g)) : "memory");
+      asm volatile("ld.shared.u16 %0, [%1];" : "=h"(y) : "r"(at + 2 * (16 * j + g + 8)) : "memory");
+      add(acc[j], t == 0 ? x : 0u, t == 0 ? y : 0u, 0u, 0u, w);
+    }
+  }
   // element of O that acc[j][0], acc[j][1] (x = 0) and acc[j][2], acc[j][3] (x = 1) stand for
-  static __device__ __forceinline__ int element(int j, int x, int g) { return D == 128 ? 64 * x + 8 * g + j : 8 * g + 4 * x + j; }
+  static __device__ __forceinline__ int element(int j, int x, int g) { return 16 * j + 8 * x + g; }
+  // O of the eight heads as rows of bf16, heads 2t and 2t + 1 times f0 and f1 (transposed, a lane holds pairs of elements of one head)
+  static __device__ __forceinline__ void leave(const float (&acc)[D / 16][4], float f0, float f1, uint32_t at, int g, int t) {
+#pragma unroll
+    for (int j = 0; j < D / 16; ++j)
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const uint32_t w = transpose8x8(round_bf16(acc[j][2 * x] * f0, acc[j][2 * x + 1] * f1));
+        asm volatile("st.shared.u32 [%0], %1;" ::"r"(at + 2 * (g * D + 16 * j + 8 * x + 2 * t)), "r"(w) : "memory");
+      }
+  }
   // the two 16-bit parts of a pair of query elements
   static __device__ __forceinline__ uint32_t high(float a, float b) { return round_bf16(a, b); }
   static __device__ __forceinline__ uint32_t low(float a, float b, uint32_t h) {
@@ -391,94 +438,123 @@ struct Rows<D, false> {
   }
 };
 
+// e4m3 numbers are multiplied as f16, which holds all of them: K rows g and g + 8, 16-byte pieces 2t, 2t + 1 of a row (D = 64: piece t);
+// V rows 2t, 2t + 1, 2t + 8, 2t + 9, the g-th eighth of a row.
 template <int D>
 struct Rows<D, true> {
-  using K = StepK8<D>;
-  using V = StepV8<D>;
-  static constexpr int kPitch = D + 8;                // rows 16 bytes apart modulo 128, pieces of a thread 32
-  static constexpr int kQ = D / 32;
-  // Weights are at most 1 and multiplied in two f16 parts, which end at 2^-24: times 2^15 they reach down to 2^-39 of the
-  // largest, so that the sum of 2^17 of the smallest is still below 2^-22 of it.
-  static constexpr float kWeight = 32768.f;
-  static __device__ __forceinline__ void load_k(K& f, const char* p, int64_t row_stride, int g, int t) {
+  static constexpr int kRowBytes = D, kSteps = kHalfUnit / (16 * kRowBytes);
+  // Weights are at most 2^kLazyLog2 and multiplied in two f16 parts, which end at 2^-24: times 2^11 they reach down to 2^-35 of
+  // the largest, so that what the sum of 2^17 of the smallest loses is still below 2^-18 of it.
+  static constexpr float kWeight = 2048.f;
+  // A step's box, as TMA leaves it: rows of 128 (64) bytes, whose 16-byte pieces are swizzled.
+  static constexpr int kStepBytes = 16 * kRowBytes;
+  static __device__ __forceinline__ uint32_t place(int row, int piece) { return row * D + ((piece ^ (D == 128 ? row & 7 : (row >> 1) & 3)) << 4); }
+  static __device__ __forceinline__ int row_of(int at) { return at / D; }
+  static __device__ __forceinline__ void load_q(uint32_t (&q)[D / 8], uint32_t row_at, int t) {
 #pragma unroll
-    for (int x = 0; x < 2; ++x)
-#pragma unroll
-      for (int i = 0; i < D / 64; ++i)
-        f.r[x][i] = load16(reinterpret_cast<const __nv_bfloat16*>(p + (g + 8 * x) * row_stride + 16 * t + 64 * i));
-  }
-  static __device__ __forceinline__ void load_v(V& f, const char* p, int64_t row_stride, int g, int t) {
-#pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      const char* row = p + (2 * t + (x & 1) + 8 * (x >> 1)) * row_stride + (D / 8) * g;
-      if constexpr (D == 128)
-        asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
-                     : "=r"(f.r[x][0]), "=r"(f.r[x][1]), "=r"(f.r[x][2]), "=r"(f.r[x][3]) : "l"(row));
-      else
-        asm volatile("ld.global.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(f.r[x][0]), "=r"(f.r[x][1]) : "l"(row));
+    for (int i = 0; i < D / 32; ++i) {                // words 8 (piece) + 2 (word of the piece) + pair
+      const uint4 x = shared16(row_at + D / 2 * t + 16 * i);
+      q[4 * i] = x.x; q[4 * i + 1] = x.y; q[4 * i + 2] = x.z; q[4 * i + 3] = x.w;
     }
   }
-  static __device__ __forceinline__ void one_row(K& fk, V& fv, const uint8_t* k_row, const uint8_t* v_row, int g, int t) {
-    const uint4 none = make_uint4(0u, 0u, 0u, 0u);
+  static __device__ __forceinline__ void mma_scores(float (&c)[4], const uint4 (&r0)[D / 64], const uint4 (&r1)[D / 64], const uint32_t (&qh)[D / 8],
+                                                    const uint32_t (&ql)[D / 8]) {
+    float p[4][4];
 #pragma unroll
-    for (int i = 0; i < D / 64; ++i) {
-      fk.r[0][i] = g == 0 ? *reinterpret_cast<const uint4*>(k_row + 16 * t + 64 * i) : none;
-      fk.r[1][i] = none;
-    }
-#pragma unroll
-    for (int x = 0; x < 4; ++x)
-#pragma unroll
-      for (int i = 0; i < D / 32; ++i)
-        fv.r[x][i] = x == 0 && t == 0 ? *reinterpret_cast<const uint32_t*>(v_row + (D / 8) * g + 4 * i) : 0u;
-  }
-  static __device__ __forceinline__ uint4 q_piece(const uint16_t* q, int t, int i) {
-    return *reinterpret_cast<const uint4*>(q + 16 * t + 64 * (i >> 1) + 8 * (i & 1));
-  }
-  static __device__ __forceinline__ void scores(float (&c)[4], const K& f, const uint4 (&q)[kQ], const uint16_t* q_low, int t) {
-    c[0] = c[1] = c[2] = c[3] = 0.f;
+    for (int x = 0; x < 4; ++x) p[x][0] = p[x][1] = p[x][2] = p[x][3] = 0.f;
 #pragma unroll
     for (int i = 0; i < D / 64; ++i)
 #pragma unroll
-      for (int w = 0; w < 4; ++w) {        // four elements of a row in each word of the piece
-        const uint32_t r0 = word_of(f.r[0][i], w), r1 = word_of(f.r[1][i], w);
-        const uint32_t a0 = f16_of_e4m3_lo(r0), a1 = f16_of_e4m3_lo(r1), a2 = f16_of_e4m3_hi(r0), a3 = f16_of_e4m3_hi(r1);
-        const uint4 h = q[2 * i + (w >> 1)], l = q_piece(q_low, t, 2 * i + (w >> 1));
-        mma16816_f16(c, a0, a1, a2, a3, (w & 1) ? l.z : l.x, (w & 1) ? l.w : l.y);
-        mma16816_f16(c, a0, a1, a2, a3, (w & 1) ? h.z : h.x, (w & 1) ? h.w : h.y);
+      for (int w = 0; w < 4; ++w) {                   // four elements of a row in each word of the piece
+        const uint32_t x0 = word_of(r0[i], w), x1 = word_of(r1[i], w);
+        const uint32_t a0 = f16_of_e4m3_lo(x0), a1 = f16_of_e4m3_lo(x1), a2 = f16_of_e4m3_hi(x0), a3 = f16_of_e4m3_hi(x1);
+        mma16816_f16(p[w & 1], a0, a1, a2, a3, qh[8 * i + 2 * w], qh[8 * i + 2 * w + 1]);
+        mma16816_f16(p[2 + (w & 1)], a0, a1, a2, a3, ql[8 * i + 2 * w], ql[8 * i + 2 * w + 1]);
       }
-  }
-  static __device__ __forceinline__ void clear(V& f, int n_real, int t) {
 #pragma unroll
-    for (int x = 0; x < 4; ++x)
-      if (2 * t + (x & 1) + 8 * (x >> 1) >= n_real) {
-#pragma unroll
-        for (int i = 0; i < D / 32; ++i) f.r[x][i] = 0u;
-      }
+    for (int x = 0; x < 4; ++x) c[x] = (p[0][x] + p[1][x]) + (p[2][x] + p[3][x]);
   }
-  // O^T += V^T P. Product j: row g is d = (D / 8) g + 2j, row g + 8 the element after it.
-  static __device__ __forceinline__ void product(Softmax<D>& s, const V& f, const float (&p)[4]) {
-    uint32_t b[2][2];
+  static __device__ __forceinline__ void scores(float (&c)[4], uint32_t at, const uint32_t (&qh)[D / 8], const uint32_t (&ql)[D / 8], int lane) {
+    uint4 r0[D / 64], r1[D / 64];
+    const int g = lane >> 2, t = lane & 3;
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) {
+      r0[i] = shared16(at + place(g, D / 64 * t + i));
+      r1[i] = shared16(at + place(g + 8, D / 64 * t + i));
+    }
+    mma_scores(c, r0, r1, qh, ql);
+  }
+  static __device__ __forceinline__ void scores_one(float (&c)[4], uint32_t at, const uint32_t (&qh)[D / 8], const uint32_t (&ql)[D / 8], int g, int t) {
+    uint4 r0[D / 64], r1[D / 64];
+    const uint4 none = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) {
+      const uint4 x = shared16(at + 16 * (D / 64 * t + i));
+      r0[i] = g == 0 ? x : none;
+      r1[i] = none;
+    }
+    mma_scores(c, r0, r1, qh, ql);
+  }
+  struct Weights { uint32_t b[2][2]; };
+  static __device__ __forceinline__ Weights weights(const float (&p)[4]) {
+    Weights w;
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
       const float p0 = p[2 * x] * kWeight, p1 = p[2 * x + 1] * kWeight;
       const __half2 h = __floats2half2_rn(p0, p1);
       const float2 back = __half22float2(h);
       const __half2 l = __floats2half2_rn(p0 - back.x, p1 - back.y);
-      b[0][x] = transpose8x8(*reinterpret_cast<const uint32_t*>(&h));
-      b[1][x] = transpose8x8(*reinterpret_cast<const uint32_t*>(&l));
+      w.b[0][x] = transpose8x8(*reinterpret_cast<const uint32_t*>(&h));
+      w.b[1][x] = transpose8x8(*reinterpret_cast<const uint32_t*>(&l));
+    }
+    return w;
+  }
+  // O^T += V^T P. Product j: row g is d = (D / 8) g + 2j, row g + 8 the element after it. r: words w of the four rows.
+  static __device__ __forceinline__ void add(float (&acc)[D / 16][4], int w, uint32_t r0, uint32_t r1, uint32_t r2, uint32_t r3, const Weights& p) {
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+      const uint32_t k0 = __byte_perm(r0, r1, y ? 0x7362 : 0x5140), k1 = __byte_perm(r2, r3, y ? 0x7362 : 0x5140);
+      const uint32_t a0 = f16_of_e4m3_lo(k0), a1 = f16_of_e4m3_hi(k0), a2 = f16_of_e4m3_lo(k1), a3 = f16_of_e4m3_hi(k1);
+      mma16816_f16(acc[2 * w + y], a0, a1, a2, a3, p.b[1][0], p.b[1][1]);
+      mma16816_f16(acc[2 * w + y], a0, a1, a2, a3, p.b[0][0], p.b[0][1]);
+    }
+  }
+  static __device__ __forceinline__ void product(float (&acc)[D / 16][4], uint32_t at, const float (&p)[4], int lane) {
+    const Weights w = weights(p);
+    const int g = lane >> 2, t = lane & 3;
+    uint4 r[4];
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const int row = 2 * t + (x & 1) + 8 * (x >> 1);
+      if constexpr (D == 128) {
+        r[x] = shared16(at + place(row, g));
+      } else {
+        const uint2 y = shared8(at + place(row, g >> 1) + 8 * (g & 1));
+        r[x] = make_uint4(y.x, y.y, 0u, 0u);
+      }
     }
 #pragma unroll
-    for (int w = 0; w < D / 32; ++w)
+    for (int n = 0; n < D / 32; ++n) add(acc, n, word_of(r[0], n), word_of(r[1], n), word_of(r[2], n), word_of(r[3], n), w);
+  }
+  static __device__ __forceinline__ void product_one(float (&acc)[D / 16][4], uint32_t at, const float (&p)[4], int g, int t) {
+    const Weights w = weights(p);
 #pragma unroll
-      for (int y = 0; y < 2; ++y) {
-        const int j = 2 * w + y;
-        const uint32_t k0 = __byte_perm(f.r[0][w], f.r[1][w], y ? 0x7362 : 0x5140), k1 = __byte_perm(f.r[2][w], f.r[3][w], y ? 0x7362 : 0x5140);
-        const uint32_t a0 = f16_of_e4m3_lo(k0), a1 = f16_of_e4m3_hi(k0), a2 = f16_of_e4m3_lo(k1), a3 = f16_of_e4m3_hi(k1);
-        mma16816_f16(s.acc[j], a0, a1, a2, a3, b[1][0], b[1][1]);
-        mma16816_f16(s.acc[j], a0, a1, a2, a3, b[0][0], b[0][1]);
-      }
+    for (int n = 0; n < D / 32; ++n) {
+      uint32_t x;
+      asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x) : "r"(at + (D / 8) * g + 4 * n) : "memory");
+      add(acc, n, t == 0 ? x : 0u, 0u, 0u, 0u, w);
+    }
   }
   static __device__ __forceinline__ int element(int j, int x, int g) { return (D / 8) * g + 2 * j + x; }
+  static __device__ __forceinline__ void leave(const float (&acc)[D / 16][4], float f0, float f1, uint32_t at, int g, int t) {
+#pragma unroll
+    for (int j = 0; j < D / 16; ++j)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t w = round_bf16(acc[j][h] * (h ? f1 : f0), acc[j][2 + h] * (h ? f1 : f0));
+        asm volatile("st.shared.u32 [%0], %1;" ::"r"(at + 2 * ((2 * t + h) * D + (D / 8) * g + 2 * j)), "r"(w) : "memory");
+      }
+  }
   static __device__ __forceinline__ uint32_t high(float a, float b) {
     const __half2 h = __floats2half2_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&h);
@@ -490,337 +566,497 @@ struct Rows<D, true> {
   }
 };
 
+// A warp's place on the line: the part of an item (prompt i, KV head kvh) that lies in its piece. An item takes kItemUnits of the line
+// more than it has units: the latencies at its beginning and end, in which its warp does not load.
+constexpr int kItemUnits = 1;
+struct Place {
+  int64_t left;                         // of the piece, from here on
+  int i, kvh;
+  int len, start;                       // rows of the prompt, first row that is read here
+  int units;                            // of an item of this prompt
+  int off, n;                           // units off .. off + n - 1 of the item
+  int used;                             // of the piece by this part
+  int next_len, next_start;             // of prompt i + 1, on their way
+};
+
+template <int kUnitRows>
+struct Line {
+  const PagedArgs& a;
+  bool fresh;
+  __device__ __forceinline__ int units(int len, int start) const { return max((len - start + kUnitRows - 1) / kUnitRows, 1); }
+  __device__ __forceinline__ void read(int i, int& len, int& start) const {
+    len = -1;
+    start = 0;
+    if (i < a.n_prompts) {
+      len = checked_length(a.c, a.lengths, i, fresh, nullptr);
+      if (a.own_start) start = a.own_start[i];
+    }
+  }
+  __device__ __forceinline__ int64_t line_units(int len, int start) const { return (int64_t)(units(len, start) + kItemUnits) * a.n_kv_heads; }
+  // `at`: place within the item
+  __device__ __forceinline__ void enter_item(Place& p, int at) const {
+    p.used = (int)min((int64_t)(p.units + kItemUnits - at), p.left);
+    p.off = max(at - kItemUnits, 0);
+    p.n = max(at + p.used - kItemUnits, 0) - p.off;
+  }
+  // `p` at prompt i (a prompt, not an idle row), `at` within what its items take of the line.
+  __device__ __forceinline__ void enter(Place& p, int64_t at) const {
+    p.units = units(p.len, p.start);
+    const int item = p.units + kItemUnits;
+    p.kvh = (int)(at / item);
+    enter_item(p, (int)(at - (int64_t)p.kvh * item));
+    read(p.i + 1, p.next_len, p.next_start);
+  }
+  __device__ __forceinline__ void advance(Place& p) const {
+    p.left -= p.used;
+    if (p.left <= 0) {
+      p.n = 0;
+      return;
+    }
+    if (++p.kvh < a.n_kv_heads) return enter_item(p, 0);
+    do {                                // (there is one: the piece is not at its end)
+      ++p.i;
+      p.len = p.next_len;
+      p.start = p.next_start;
+      if (p.len < 0) read(p.i + 1, p.next_len, p.next_start);
+    } while (p.len < 0);
+    enter(p, 0);
+  }
+};
+
 template <int D, bool kE4m3>
-__global__ void __launch_bounds__(kPagedThreads, D == 128 ? 3 : 4)
-paged_decode_kernel(const __grid_constant__ PagedArgs a) {
+__global__ void __launch_bounds__(kStepThreads, 1)
+paged_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ PagedArgs a,
+                    const __grid_constant__ SharedPlan plan) {
   using R = Rows<D, kE4m3>;
-  constexpr int kHalf = D / 2, kSize = kE4m3 ? 1 : 2;
-  extern __shared__ int32_t s_ptr[];                                       // [k + 1]
-  __shared__ int64_t s_warp[kPagedWarps];
-  __shared__ float s_cos[kHalf], s_sin[kHalf];
-  __shared__ __align__(16) uint16_t s_q[2][kMaxGroup][R::kPitch];          // rotated queries, upper and lower part
-  __shared__ __align__(16) uint8_t s_new[2][D * kSize];                    // the new token's rows of the pages
-  __shared__ float s_scale[kMaxGroup];                                     // to scaled log2 units
-  __shared__ float s_m[kPagedWarps][kMaxGroup], s_l[kPagedWarps][kMaxGroup];
-  __shared__ float s_o[kPagedWarps][kMaxGroup][D];
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
-  const bool fresh = a.k_new != nullptr;
+  constexpr int kSteps = R::kSteps, kUnitRows = 16 * kSteps, kHalf = D / 2, kSize = kE4m3 ? 1 : 2;
+  constexpr int kLanesPerHead = kHalf / 4, kHeadsAtOnce = 32 / kLanesPerHead;       // queries: four (j, j + D/2) pairs a lane
+  constexpr int kQPitch = 2 * D + 16;                                               // bytes
+  static_assert(kMaxGroup * kQPitch <= kScratch && kMaxGroup * D * 2 <= kScratch && 4 * D <= kScratch, "scratch");
+  extern __shared__ __align__(1024) uint8_t s_dyn[];
+  __shared__ int64_t s_warp[kStepWarps], s_before[kStepThreads];
+  __shared__ uint64_t s_bar[kStepWarps][4];                 // K of two units, V of two units
+  __shared__ int s_abort;
+  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31, g = lane >> 2, t = lane & 3;
+  const Line<kUnitRows> line{a, a.k_new != nullptr};
+  const bool fresh = line.fresh;
+  const uint32_t bars = smem_u32(s_bar[warp]);
+  if (lane == 0) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) mbar_init(bars + 8 * i, 1);
+    s_abort = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  const WaitCtx wctx{smem_u32(&s_abort), a.wait_limit, a.status};
   pdl_wait();                           // lengths, table, pages: all may come from the kernel before
   pdl_launch_dependents();
-  const int chunk_blocks = cut_into_chunks(a, s_ptr, s_warp);
-  const int n_chunks_all = s_ptr[a.n_prompts];
-  if (blockIdx.x == 0)
-    for (int i = tid; i <= a.n_prompts; i += kPagedThreads) a.chunk_ptr[i] = s_ptr[i];
 
-  const int64_t n_work = (int64_t)n_chunks_all * a.n_kv_heads;
-  for (int64_t work = blockIdx.x; work < n_work; work += gridDim.x) {
-    const int chunk = (int)(work / a.n_kv_heads), kvh = (int)(work - (int64_t)chunk * a.n_kv_heads);
-    int lo = 0, hi = a.n_prompts - 1;   // last prompt whose first chunk is <= chunk (the prompts without any come before it)
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (s_ptr[mid] <= chunk) lo = mid; else hi = mid - 1;
+  // ---- the line, and this warp's piece of it
+  const int each = (a.n_prompts + kStepThreads - 1) / kStepThreads;
+  int64_t mine = 0, total;
+  for (int i = tid * each; i < min((tid + 1) * each, a.n_prompts); ++i) {
+    const int len = checked_length(a.c, a.lengths, i, fresh, blockIdx.x == 0 ? a.status : nullptr);
+    if (len >= 0) mine += line.line_units(len, a.own_start ? a.own_start[i] : 0);
+  }
+  s_before[tid] = block_prefix<kStepThreads>(mine, s_warp, total);
+  __syncthreads();
+  const int64_t per = (total + kPieces - 1) / kPieces;
+  const int piece = warp * kSms + blockIdx.x;               // few units: a warp on each SM first
+  const int64_t u0 = piece * per;
+  Place c;                              // where the arithmetic is
+  c.left = min(per, total - u0);
+  if (lane == 0) a.cut[piece] = make_int4(0, 0, 0, 0);
+  if (c.left <= 0) return;
+  {
+    int lo = 0;                         // last thread whose prompts begin at or before u0 (those without units come before it)
+    for (int w = 0; w < kStepWarps; ++w) lo += __popc(__ballot_sync(0xffffffffu, s_before[32 * w + lane] <= u0));
+    --lo;
+    int64_t at = u0 - s_before[lo];
+    c.i = lo * each;
+    for (;; ++c.i) {
+      line.read(c.i, c.len, c.start);
+      const int64_t here = c.len < 0 ? 0 : line.line_units(c.len, c.start);
+      if (at < here) break;
+      at -= here;
     }
-    const int i = lo, c0 = s_ptr[i], n_chunks = s_ptr[i + 1] - c0, len = a.lengths[i];
-    const int start = a.own_start ? a.own_start[i] : 0;
-    const int64_t chunk_keys = (int64_t)chunk_blocks * kBlockKeys;
-    const int key0 = (int)min(start + (chunk - c0) * chunk_keys, (int64_t)len), key_end = (int)min(key0 + chunk_keys, (int64_t)len);
-    const bool last_chunk = chunk - c0 == n_chunks - 1;
-    const int32_t* table = a.c.table + (int64_t)i * a.c.table_stride;
-    const int64_t head_at = (int64_t)kvh * a.c.head_stride;
-    // Pages of this warp's steps (key0 + 16 * (warp + 4n)), 32 at a time, one per lane.
-    const int first = key0 + kStepKeys * warp;
-    auto page_ids = [&](int n0) {
-      const int64_t key = first + (int64_t)(n0 + lane) * kBlockKeys;
-      int id = 0;
-      if (key < key_end) {
-        id = table[key >> a.c.page_shift];
-        if ((unsigned)id >= (unsigned)a.c.n_pages) {
-          note_status(a.status, PP_PAGED_BAD_PAGE);
-          id = 0;
-        }
-      }
-      return id;
-    };
-    int ids = page_ids(0), ids_next = 0;
-    const int row_mask = (1 << a.c.page_shift) - 1;
-    auto offset = [&](int n, int key) {
-      return (int64_t)__shfl_sync(0xffffffffu, ids, n & 31) * a.c.page_stride + head_at + (int64_t)(key & row_mask) * a.c.row_stride;
-    };
+    line.enter(c, at);
+    if (c.n == 0) line.advance(c);      // a piece that ends before the item's first unit leaves it to the next
+    if (c.n == 0) return;
+  }
 
-    // queries of the group and the new key, four (j, j + D/2) pairs at a time, zeros for absent heads
-    constexpr int kUnits = kHalf / 4, kRotUnits = (kMaxGroup + 1) * kUnits, kTrips = (kRotUnits + kPagedThreads - 1) / kPagedThreads;
-    uint2 lo2[kTrips], hi2[kTrips];
+  // ---- loads, which run ahead
+  const uint32_t aligned = (smem_u32(s_dyn) + 1023u) & ~1023u;
+  const uint32_t ring = aligned + warp * (4 * kHalfUnit);                           // K of two units, V of two units
+  uint8_t* scratch_p = s_dyn + (aligned - smem_u32(s_dyn)) + kStepWarps * (4 * kHalfUnit) + warp * kScratch;
+  const uint32_t scratch = smem_u32(scratch_p), issue = elect_one(), lane_issue = lane < kSteps ? 1u : 0u;
+  const int row_mask = (1 << a.c.page_shift) - 1;
+  Place f = c;                          // where the copies are: unit f_at of the part f
+  int f_at = 0, f_batch = -1, ids = 0, ids_prompt = -1;
+  // Pages of the steps of an item, 32 at a time, one per lane; the next head of a prompt starts with the same ones.
+  auto pages_of = [&](int batch) {
+    if (ids_prompt == f.i && f_batch == batch) return;
+    f_batch = batch;
+    ids_prompt = f.i;
+    const int64_t row = f.start + ((int64_t)batch * 32 + lane) * 16;
+    ids = 0;
+    if (row < f.len) {
+      ids = a.c.table[(int64_t)f.i * a.c.table_stride + (row >> a.c.page_shift)];
+      if ((unsigned)ids >= (unsigned)a.c.n_pages) {
+        note_status(a.status, PP_PAGED_BAD_PAGE);
+        ids = 0;
+      }
+    }
+  };
+  uint32_t stage_f = 0;                 // stage that the next unit goes to
+  auto load_half = [&](int v) {         // a lane for each step of the unit
+    const int unit = f.off + f_at, step = unit * kSteps + lane, row = f.start + step * 16;
+    pages_of(unit * kSteps >> 5);
+    const int id = __shfl_sync(0xffffffffu, ids, step & 31);
+    const uint32_t bar = bars + 8 * (2 * v + stage_f), to = ring + (2 * v + stage_f) * kHalfUnit;
+    mbar_expect_tx(bar, kHalfUnit, issue);
+    __syncwarp();
+    load_rows(to + lane * R::kStepBytes, v ? &map_v : &map_k, bar, row & row_mask, f.kvh, row < f.len ? id : a.c.n_pages, lane_issue);
+  };
+  auto load_k = [&]() {                 // (f.n = 0: nothing is left)
+    if (f.n > 0) load_half(0);
+  };
+  auto load_v = [&]() {                 // and on to the next unit
+    if (f.n == 0) return;
+    load_half(1);
+    stage_f ^= 1;
+    if (++f_at == f.n) {
+      line.advance(f);
+      f_at = 0;
+    }
+  };
+  load_k();
+  load_v();
+  load_k();
+  load_v();
+
+  uint32_t stage = 0, phase = 0;
+  int angles_of = -1;
+  float cs[4], sn[4];                   // of this lane's four pairs, at the position of prompt angles_of
+  const int j0 = 4 * (lane % kLanesPerHead);
+  // A wait gave up: loads of this warp may still be in flight. They get time to land before shared memory is handed back.
+  auto settle = [&]() {
+    const unsigned long long t0 = global_ns();
+    while (global_ns() - t0 < 100000ull) {}
+  };
+  while (true) {
+    // ---- a part of an item: queries
+    const bool begins = c.off == 0, ends = c.off + c.n == c.units, new_row = ends && fresh;
+    const __nv_bfloat16* q_row = a.q_new + (int64_t)c.i * a.q_stride + (int64_t)c.kvh * a.group * D;
+    uint2 lo2[kMaxGroup / kHeadsAtOnce], hi2[kMaxGroup / kHeadsAtOnce], new_lo, new_hi, new_v;
 #pragma unroll
-    for (int x = 0; x < kTrips; ++x) {
-      const int u = tid + x * kPagedThreads, h = u / kUnits, j = 4 * (u - h * kUnits);
+    for (int x = 0; x < kMaxGroup / kHeadsAtOnce; ++x) {
+      const int h = x * kHeadsAtOnce + lane / kLanesPerHead;
       lo2[x] = hi2[x] = make_uint2(0u, 0u);
-      if (h < a.group || (h == kMaxGroup && last_chunk && fresh)) {
-        const __nv_bfloat16* src = h == kMaxGroup ? a.k_new + (int64_t)i * a.k_stride + kvh * D
-                                                  : a.q_new + (int64_t)i * a.q_stride + (kvh * a.group + h) * D;
-        lo2[x] = *reinterpret_cast<const uint2*>(src + j);
-        hi2[x] = *reinterpret_cast<const uint2*>(src + j + kHalf);
+      if (h < a.group) {
+        lo2[x] = *reinterpret_cast<const uint2*>(q_row + h * D + j0);
+        hi2[x] = *reinterpret_cast<const uint2*>(q_row + h * D + j0 + kHalf);
       }
     }
-    uint2 v_mine = make_uint2(0u, 0u);
-    const bool v_here = last_chunk && fresh && tid < D / 4;
-    if (v_here) v_mine = *reinterpret_cast<const uint2*>(a.v_new + (int64_t)i * a.v_stride + kvh * D + 4 * tid);
-    typename R::K fk;
-    typename R::V fv;
-    int key = first, n = 0;
-    if (key < key_end) {
-      const int64_t at = offset(0, key);
-      R::load_k(fk, a.c.k_pages + at, a.c.row_stride, g, t);
-      R::load_v(fv, a.c.v_pages + at, a.c.row_stride, g, t);
+    if (new_row) {
+      const __nv_bfloat16* k_row = a.k_new + (int64_t)c.i * a.k_stride + c.kvh * D;
+      new_lo = *reinterpret_cast<const uint2*>(k_row + j0);
+      new_hi = *reinterpret_cast<const uint2*>(k_row + j0 + kHalf);
+      new_v = *reinterpret_cast<const uint2*>(a.v_new + (int64_t)c.i * a.v_stride + c.kvh * D + 4 * (lane % (D / 4)));
     }
-    if (tid < kHalf) angle(fresh ? len : max(len - 1, 0), a.angles.inv_freq[tid], s_cos[tid], s_sin[tid]);
-    __syncthreads();
-    const float k_scale = kE4m3 ? a.c.k_scale[kvh] : 1.f, v_scale = kE4m3 ? a.c.v_scale[kvh] : 1.f;
+    // (m, l) and o over the rows that the prompt shares, where this part is the item's first
+    float m[2] = {kNoScore, kNoScore}, l[2] = {0.f, 0.f}, acc[D / 16][4];
 #pragma unroll
-    for (int x = 0; x < kTrips; ++x) {
-      const int u = tid + x * kPagedThreads, h = u / kUnits, j = 4 * (u - h * kUnits);
-      float p[4], y[4];
-      {
-        const float2 p0 = unpack_bf16(lo2[x].x), p1 = unpack_bf16(lo2[x].y), y0 = unpack_bf16(hi2[x].x), y1 = unpack_bf16(hi2[x].y);
-        p[0] = p0.x; p[1] = p0.y; p[2] = p1.x; p[3] = p1.y;
-        y[0] = y0.x; y[1] = y0.y; y[2] = y1.x; y[3] = y1.y;
+    for (int j = 0; j < D / 16; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.f;
+    if (begins && c.start > 0) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int head = 2 * t + h;
+        if (head >= a.group) continue;
+        const int64_t at = (int64_t)c.i * a.n_q_heads + c.kvh * a.group + head;
+        const float2 ml = plan.row_ml[at];
+        m[h] = ml.x;
+        l[h] = g == 0 ? ml.y : 0.f;
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j)
+#pragma unroll
+          for (int x = 0; x < 2; ++x) acc[j][2 * x + h] = plan.row_o[at * D + R::element(j, x, g)];
       }
-      int shift = 0;
+    }
+    if (angles_of != c.i) {
+      angles_of = c.i;
+      angles4(fresh ? c.len : max(c.len - 1, 0), a.angles.inv_freq + j0, cs, sn);
+    }
+    auto turn = [&](uint2 lo, uint2 hi, float (&p)[4], float (&y)[4]) {
+      const float2 p0 = unpack_bf16(lo.x), p1 = unpack_bf16(lo.y), y0 = unpack_bf16(hi.x), y1 = unpack_bf16(hi.y);
+      const float x[4] = {p0.x, p0.y, p1.x, p1.y}, z[4] = {y0.x, y0.y, y1.x, y1.y};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        p[e] = turn_lo(x[e], z[e], cs[e], sn[e]);
+        y[e] = turn_hi(x[e], z[e], cs[e], sn[e]);
+      }
+    };
+    const float k_scale = kE4m3 ? a.c.k_scale[c.kvh] : 1.f, v_scale = kE4m3 ? a.c.v_scale[c.kvh] : 1.f;
+    uint32_t qh[D / 8], ql[D / 8];
+    float scale[2] = {a.scale_log2, a.scale_log2};
+    // the upper parts through the scratch memory, then the lower ones, which wait in lo2 and hi2
+#pragma unroll
+    for (int x = 0; x < kMaxGroup / kHeadsAtOnce; ++x) {
+      if (x * kHeadsAtOnce >= a.group) break;
+      const int h = x * kHeadsAtOnce + lane / kLanesPerHead;
+      float p[4], y[4];
+      turn(lo2[x], hi2[x], p, y);
       if constexpr (kE4m3) {
-        // f16 has 5 exponent bits: a query is brought to below 2 by a power of two, which goes into its factor
+        // f16 has 5 exponent bits: a query is brought to below 2 by a power of two (of up to 2^120: the rest f16 has room
+        // for), which goes into its factor
         float top = 0.f;
 #pragma unroll
         for (int e = 0; e < 4; ++e) top = fmaxf(top, fmaxf(fabsf(p[e]), fabsf(y[e])));
 #pragma unroll
-        for (int o = kUnits / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-        if (top > 0.f && top < INFINITY) shift = ilogbf(top) + 1;
-      }
+        for (int o = kLanesPerHead / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        const int shift = min(max((int)(__float_as_uint(top) >> 23) - 127, -120), 120);
+        const float down = __uint_as_float((uint32_t)(127 - shift) << 23), factor = a.scale_log2 * k_scale * __uint_as_float((uint32_t)(127 + shift) << 23);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float cs = s_cos[j + e], sn = s_sin[j + e], pe = p[e], ye = y[e];
-        p[e] = turn_lo(pe, ye, cs, sn);
-        y[e] = turn_hi(pe, ye, cs, sn);
-      }
-      if (h < kMaxGroup) {
-        if constexpr (kE4m3) {
+        for (int e = 0; e < 4; ++e) { p[e] *= down; y[e] *= down; }
 #pragma unroll
-          for (int e = 0; e < 4; ++e) { p[e] = scalbnf(p[e], -shift); y[e] = scalbnf(y[e], -shift); }
-        }
-        if (j == 0) s_scale[h] = scalbnf(a.scale_log2 * k_scale, shift);
-        const uint32_t ph[2] = {R::high(p[0], p[1]), R::high(p[2], p[3])}, yh[2] = {R::high(y[0], y[1]), R::high(y[2], y[3])};
-        *reinterpret_cast<uint2*>(&s_q[0][h][j]) = make_uint2(ph[0], ph[1]);
-        *reinterpret_cast<uint2*>(&s_q[0][h][j + kHalf]) = make_uint2(yh[0], yh[1]);
-        *reinterpret_cast<uint2*>(&s_q[1][h][j]) = make_uint2(R::low(p[0], p[1], ph[0]), R::low(p[2], p[3], ph[1]));
-        *reinterpret_cast<uint2*>(&s_q[1][h][j + kHalf]) = make_uint2(R::low(y[0], y[1], yh[0]), R::low(y[2], y[3], yh[1]));
-      } else if (h == kMaxGroup) {
-        if constexpr (kE4m3) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) { p[e] = __fdiv_rn(p[e], k_scale); y[e] = __fdiv_rn(y[e], k_scale); }
-          *reinterpret_cast<uint32_t*>(&s_new[0][j]) = round_e4m3(p[0], p[1], p[2], p[3]);
-          *reinterpret_cast<uint32_t*>(&s_new[0][j + kHalf]) = round_e4m3(y[0], y[1], y[2], y[3]);
-        } else {
-          *reinterpret_cast<uint2*>(&s_new[0][2 * j]) = make_uint2(round_bf16(p[0], p[1]), round_bf16(p[2], p[3]));
-          *reinterpret_cast<uint2*>(&s_new[0][2 * (j + kHalf)]) = make_uint2(round_bf16(y[0], y[1]), round_bf16(y[2], y[3]));
+        for (int z = 0; z < 2; ++z) {       // heads 2t and 2t + 1 are this lane's columns
+          const float other = __shfl_sync(0xffffffffu, factor, ((2 * t + z) % kHeadsAtOnce) * kLanesPerHead);
+          if ((2 * t + z) / kHeadsAtOnce == x) scale[z] = other;
         }
       }
+      const uint32_t w[4] = {R::high(p[0], p[1]), R::high(p[2], p[3]), R::high(y[0], y[1]), R::high(y[2], y[3])};
+      *reinterpret_cast<uint2*>(scratch_p + h * kQPitch + 2 * j0) = make_uint2(w[0], w[1]);
+      *reinterpret_cast<uint2*>(scratch_p + h * kQPitch + 2 * (j0 + kHalf)) = make_uint2(w[2], w[3]);
+      lo2[x] = make_uint2(R::low(p[0], p[1], w[0]), R::low(p[2], p[3], w[1]));
+      hi2[x] = make_uint2(R::low(y[0], y[1], w[2]), R::low(y[2], y[3], w[3]));
     }
-    if (v_here) {
-      if constexpr (kE4m3) {
-        const float2 x = unpack_bf16(v_mine.x), y = unpack_bf16(v_mine.y);
-        *reinterpret_cast<uint32_t*>(&s_new[1][4 * tid]) = round_e4m3(__fdiv_rn(x.x, v_scale), __fdiv_rn(x.y, v_scale), __fdiv_rn(y.x, v_scale), __fdiv_rn(y.y, v_scale));
-      } else {
-        *reinterpret_cast<uint2*>(&s_new[1][8 * tid]) = v_mine;
-      }
-    }
-    __syncthreads();
-    uint4 q[R::kQ];
+    __syncwarp();
+    R::load_q(qh, scratch + g * kQPitch, t);
+    __syncwarp();
 #pragma unroll
-    for (int x = 0; x < R::kQ; ++x) q[x] = R::q_piece(s_q[0][g], t, x);
-    const uint16_t* q_low = s_q[1][g];
-    const float scale[2] = {s_scale[2 * t], s_scale[2 * t + 1]};
+    for (int x = 0; x < kMaxGroup / kHeadsAtOnce; ++x) {
+      if (x * kHeadsAtOnce >= a.group) break;
+      const int h = x * kHeadsAtOnce + lane / kLanesPerHead;
+      *reinterpret_cast<uint2*>(scratch_p + h * kQPitch + 2 * j0) = lo2[x];
+      *reinterpret_cast<uint2*>(scratch_p + h * kQPitch + 2 * (j0 + kHalf)) = hi2[x];
+    }
+    __syncwarp();
+    R::load_q(ql, scratch + g * kQPitch, t);
+    __syncwarp();
+    if (g >= a.group) {                 // absent heads
+#pragma unroll
+      for (int x = 0; x < D / 8; ++x) qh[x] = ql[x] = 0u;
+    }
 
-    Softmax<D> s;
+    // ---- the rows
+    // Weights of the scores in s (rows at or past n_real are hidden), with O, l and m brought to the new maximum.
+    auto soften = [&](auto& s, int n_real) {
+      constexpr int kN = sizeof(s) / sizeof(s[0]);
+      if (n_real < 16 * kN) {
 #pragma unroll
-    for (int j = 0; j < D / 16; ++j)
+        for (int x = 0; x < kN; ++x)
 #pragma unroll
-      for (int x = 0; x < 4; ++x) s.acc[j][x] = 0.f;
-    float c[4];
-    // K of the next step is loaded as soon as the scores of this one are there, V after its product.
-    while (key < key_end) {
-      R::scores(c, fk, q, q_low, t);
-      const int next = key + kBlockKeys;
-      const bool more = next < key_end;
-      int64_t at = 0;
-      if (more) {
-        ++n;
-        if ((n & 31) == 16) ids_next = page_ids((n & ~31) + 32);
-        if ((n & 31) == 0) ids = ids_next;
-        at = offset(n, next);
-        R::load_k(fk, a.c.k_pages + at, a.c.row_stride, g, t);
+          for (int y = 0; y < 4; ++y)
+            if (16 * x + g + 8 * (y >> 1) >= n_real) s[x][y] = -INFINITY;
       }
-      softmax_step<D>(s, c, scale, key_end - key, g);
-      if (key_end - key < kStepKeys) R::clear(fv, key_end - key, t);
-      R::product(s, fv, c);
-      if (more) R::load_v(fv, a.c.v_pages + at, a.c.row_stride, g, t);
-      key = next;
+      float mx[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+      for (int x = 0; x < kN; ++x)
+#pragma unroll
+        for (int y = 0; y < 4; ++y) mx[y & 1] = fmaxf(mx[y & 1], s[x][y]);
+      mx[0] *= scale[0];
+      mx[1] *= scale[1];
+      if (__any_sync(0xffffffffu, mx[0] > m[0] + kLazyLog2 || mx[1] > m[1] + kLazyLog2)) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+          for (int o = 4; o < 32; o <<= 1) mx[h] = fmaxf(mx[h], __shfl_xor_sync(0xffffffffu, mx[h], o));
+          const float m_new = fmaxf(m[h], mx[h]), alpha = ex2(m[h] - m_new);         // 0 on the first step
+          m[h] = m_new;
+          l[h] *= alpha;
+#pragma unroll
+          for (int j = 0; j < D / 16; ++j) { acc[j][h] *= alpha; acc[j][2 + h] *= alpha; }
+        }
+      }
+#pragma unroll
+      for (int x = 0; x < kN; ++x)
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          s[x][y] = ex2(__fmaf_rn(s[x][y], scale[y & 1], -m[y & 1]));
+          l[y & 1] += s[x][y];
+        }
+    };
+    int row0 = c.start + c.off * kUnitRows;
+    for (int n = 0; n < c.n; ++n, row0 += kUnitRows) {
+      float s[kSteps][4];
+      const uint32_t k_at = ring + stage * kHalfUnit, v_at = k_at + 2 * kHalfUnit;
+      if (!mbar_wait_issuer<kWaitRows>(bars + 8 * stage, phase, wctx)) return settle();
+#pragma unroll
+      for (int x = 0; x < kSteps; ++x) R::scores(s[x], k_at + x * R::kStepBytes, qh, ql, lane);
+      __syncwarp();
+      load_k();
+      const int n_real = c.len - row0;
+      soften(s, n_real);
+      if (!mbar_wait_issuer<kWaitRows>(bars + 16 + 8 * stage, phase, wctx)) return settle();
+      if (n_real < kUnitRows) {
+        // The rows past the last one are of no part of O, not as 0 times what they hold either.
+        for (int at = 16 * lane; at < kHalfUnit; at += 16 * 32)
+          if (R::row_of(at) >= n_real) asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(v_at + at), "r"(0) : "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+      }
+#pragma unroll
+      for (int x = 0; x < kSteps; ++x) R::product(acc, v_at + x * R::kStepBytes, s[x], lane);
+      __syncwarp();
+      load_v();
+      stage ^= 1;
+      phase ^= stage ^ 1;               // (after every second unit)
     }
-    if (last_chunk && fresh && warp == 0) {        // the new token, and its rows of the pages
-      R::one_row(fk, fv, s_new[0], s_new[1], g, t);
-      R::scores(c, fk, q, q_low, t);
-      softmax_step<D>(s, c, scale, 1, g);
-      R::product(s, fv, c);
-      const int page = table[len >> a.c.page_shift];
+    if (new_row) {                      // the new token, and its rows of the pages
+      float p[4], y[4];
+      turn(new_lo, new_hi, p, y);
+      const float2 v0 = unpack_bf16(new_v.x), v1 = unpack_bf16(new_v.y);
+      if constexpr (kE4m3) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { p[e] = __fdiv_rn(p[e], k_scale); y[e] = __fdiv_rn(y[e], k_scale); }
+        if (lane < kLanesPerHead) {
+          *reinterpret_cast<uint32_t*>(scratch_p + j0) = round_e4m3(p[0], p[1], p[2], p[3]);
+          *reinterpret_cast<uint32_t*>(scratch_p + j0 + kHalf) = round_e4m3(y[0], y[1], y[2], y[3]);
+        }
+        if (lane < D / 4)
+          *reinterpret_cast<uint32_t*>(scratch_p + D + 4 * lane) =
+              round_e4m3(__fdiv_rn(v0.x, v_scale), __fdiv_rn(v0.y, v_scale), __fdiv_rn(v1.x, v_scale), __fdiv_rn(v1.y, v_scale));
+      } else {
+        if (lane < kLanesPerHead) {
+          *reinterpret_cast<uint2*>(scratch_p + 2 * j0) = make_uint2(round_bf16(p[0], p[1]), round_bf16(p[2], p[3]));
+          *reinterpret_cast<uint2*>(scratch_p + 2 * (j0 + kHalf)) = make_uint2(round_bf16(y[0], y[1]), round_bf16(y[2], y[3]));
+        }
+        if (lane < D / 4) *reinterpret_cast<uint2*>(scratch_p + 2 * D + 8 * lane) = new_v;
+      }
+      __syncwarp();
+      float s[1][4];
+      R::scores_one(s[0], scratch, qh, ql, g, t);
+      soften(s, 1);
+      R::product_one(acc, scratch + D * kSize, s[0], g, t);
+      const int page = a.c.table[(int64_t)c.i * a.c.table_stride + (c.len >> a.c.page_shift)];
       if ((unsigned)page < (unsigned)a.c.n_pages) {
-        const int64_t at = (int64_t)page * a.c.page_stride + head_at + (int64_t)(len & row_mask) * a.c.row_stride;
-        if (lane < D * kSize / 16) {
-          *reinterpret_cast<uint4*>(a.c.k_pages + at + 16 * lane) = *reinterpret_cast<const uint4*>(&s_new[0][16 * lane]);
-          *reinterpret_cast<uint4*>(a.c.v_pages + at + 16 * lane) = *reinterpret_cast<const uint4*>(&s_new[1][16 * lane]);
+        const int64_t to = (int64_t)page * a.c.page_stride + (int64_t)c.kvh * a.c.head_stride + (int64_t)(c.len & row_mask) * a.c.row_stride;
+        if (lane < R::kRowBytes / 16) {
+          *reinterpret_cast<uint4*>(a.c.k_pages + to + 16 * lane) = shared16(scratch + 16 * lane);
+          *reinterpret_cast<uint4*>(a.c.v_pages + to + 16 * lane) = shared16(scratch + D * kSize + 16 * lane);
         }
       } else if (lane == 0) {
         note_status(a.status, PP_PAGED_BAD_PAGE);
       }
+      __syncwarp();
     }
-    // merge the four warps (one without keys has m = kNoScore, l = 0)
+
+    // ---- out
+    const float out_scale = v_scale / R::kWeight;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      float l = s.l[h];
+    for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int o = 4; o < 32; o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
-      const int head = 2 * t + h;
-      if (head < a.group) {
-        if (g == 0) { s_m[warp][head] = s.m[h]; s_l[warp][head] = l; }
+      for (int o = 4; o < 32; o <<= 1) l[h] += __shfl_xor_sync(0xffffffffu, l[h], o);
+    if (begins && ends) {
+      // (a row that attends to nothing is 0; one all of whose scores are -inf is a NaN)
+      const bool none = c.len + (int)fresh <= 0;
+      R::leave(acc, none ? 0.f : out_scale / l[0], none ? 0.f : out_scale / l[1], scratch, g, t);
+      __syncwarp();
+      __nv_bfloat16* to = a.o + ((int64_t)c.i * a.n_q_heads + c.kvh * a.group) * D;
+      for (int x = lane; x < a.group * D / 8; x += 32) *reinterpret_cast<uint4*>(to + 8 * x) = shared16(scratch + 16 * x);
+      __syncwarp();
+    } else {
+      const int64_t slot = 2 * (int64_t)piece + (begins ? 1 : 0);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int head = 2 * t + h;
+        if (head >= a.group) continue;
+        if (g == 0) a.part_ml[slot * a.group + head] = make_float2(m[h], l[h]);
+        float* to = a.part_o + (slot * a.group + head) * D;
 #pragma unroll
         for (int j = 0; j < D / 16; ++j)
 #pragma unroll
-          for (int x = 0; x < 2; ++x) s_o[warp][head][R::element(j, x, g)] = s.acc[j][2 * x + h];
+          for (int x = 0; x < 2; ++x) to[R::element(j, x, g)] = acc[j][2 * x + h] * out_scale;
       }
+      if (begins && lane == 0)          // the pieces over which the item goes on: units behind this one's end
+        a.cut[piece] = make_int4(c.i, c.kvh, 1 + (int)((c.units - c.n + per - 1) / per), 0);
     }
-    __syncthreads();
-    const float out_scale = v_scale / R::kWeight;
-    for (int u = tid; u < a.group * D; u += kPagedThreads) {
-      const int h = u / D, d = u - h * D;
-      float mm = s_m[0][h];
-#pragma unroll
-      for (int w = 1; w < kPagedWarps; ++w) mm = fmaxf(mm, s_m[w][h]);
-      float ll = 0.f, oo = 0.f;
-#pragma unroll
-      for (int w = 0; w < kPagedWarps; ++w) {
-        const float f = ex2(s_m[w][h] - mm);
-        ll += s_l[w][h] * f;
-        oo += s_o[w][h][d] * f;
-      }
-      oo *= out_scale;
-      const int head = kvh * a.group + h;
-      if (n_chunks == 1 && !a.own_start) {
-        // (a row that attends to nothing is 0; one all of whose scores are -inf is a NaN)
-        a.o[((int64_t)i * a.n_q_heads + head) * D + d] = __float2bfloat16_rn(len + (int)fresh > 0 ? oo / ll : 0.f);
-      } else {
-        const int64_t at = (int64_t)chunk * a.n_q_heads + head;
-        if (d == 0) a.part_ml[at] = make_float2(mm, ll);
-        a.part_o[at * D + d] = oo;
-      }
-    }
-    __syncthreads();
+    line.advance(c);
+    if (c.n == 0) return;
   }
 }
 
-// Joins the parts of every (prompt, query head): the chunks of the prompt's own rows and, with a plan, the pieces of the
-// shared ones. kAcross = false: one warp for a head, four heads in a CTA. true: four warps for a head, for few (prompt,
-// head) pairs, of which one may have hundreds of parts.
-template <int D, bool kAcross>
-__global__ void __launch_bounds__(kPagedThreads)
-paged_combine_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ SharedPlan plan) {
-  constexpr int E = D / 32;             // consecutive elements per lane
-  __shared__ float s_m[kPagedWarps], s_l[kPagedWarps], s_o[kPagedWarps][D];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int i = blockIdx.x, head = kAcross ? blockIdx.y : blockIdx.y * kPagedWarps + warp;
-  const bool fresh = a.k_new != nullptr;
-  pdl_wait();                           // the partial results come from the kernels before this one
+// Joins the parts of the items that are cut: a CTA for a query head of the KV head, which takes every kCombineBlocks-th piece in which
+// such an item may begin. Its warps share the parts: one prompt alone may have hundreds.
+template <int D>
+__global__ void __launch_bounds__(kCombineThreads)
+paged_combine_kernel(const __grid_constant__ PagedArgs a) {
+  constexpr int E = D / 32, kWarps = kCombineThreads / 32;      // E: consecutive elements per lane
+  __shared__ float s_m[kWarps], s_l[kWarps], s_o[kWarps][D];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, h = blockIdx.y;
+  pdl_wait();                           // the parts come from the kernels before this one
   pdl_launch_dependents();
-  if (!kAcross && head >= a.n_q_heads) return;
-  const int c0 = a.chunk_ptr[i], n_own = a.chunk_ptr[i + 1] - c0;
-  if (n_own == 0 || (n_own == 1 && !a.own_start)) return;      // a row of no prompt; one whose O is complete
-  const int len = a.lengths[i];
-  const float2* ml_own = a.part_ml + (int64_t)c0 * a.n_q_heads + head;
-  const float* o_own = a.part_o + ((int64_t)c0 * a.n_q_heads + head) * D;
-  const float2* ml_shared = nullptr;
-  const float* o_shared = nullptr;
-  int n_shared = 0;
-  if (a.own_start) {
-    const int gr = plan.group_of[i], tiles = gr >= 0 ? plan.key_tiles[gr] : 0;
-    if (tiles > 0) {
-      const int first = plan.group_ptr[gr], rows = (plan.group_ptr[gr + 1] - first) * a.group;
-      const int kvh = head / a.group, row = (i - first) * a.group + head - kvh * a.group, rt = row / kSharedTileRows;
-      const int64_t per = units_per_piece(*plan.units, plan.n_ctas);
-      const int64_t u0 = plan.unit_start[gr] + ((int64_t)kvh * ((rows + kSharedTileRows - 1) / kSharedTileRows) + rt) * tiles;
-      const int p0 = (int)(u0 / per);
-      n_shared = (int)((u0 + tiles - 1) / per) - p0 + 1;
-      const int64_t at = (int64_t)p0 * kSharedTileRows + ((int64_t)(first - plan.group_ptr[0]) * a.n_kv_heads * a.group) + (int64_t)kvh * rows + row;
-      ml_shared = plan.ml + at;
-      o_shared = plan.o + at * D;
-    }
-  }
-  float mm = kNoScore, ll = 0.f, oo[E];
+  for (int piece = blockIdx.x; piece < kPieces; piece += kCombineBlocks) {
+    const int4 cut = a.cut[piece];
+    if (cut.z == 0) continue;
+    float mm = kNoScore, ll = 0.f, oo[E];
 #pragma unroll
-  for (int e = 0; e < E; ++e) oo[e] = 0.f;
-  const int n_all = n_own + n_shared, step = kAcross ? kPagedWarps : 1;
-  for (int base = kAcross ? warp : 0; base < n_all; base += 32 * step) {      // 32 parts at a time: one (m, l) per lane
-    const int n = min(32, (n_all - base + step - 1) / step), mine = base + lane * step;
-    float2 ml = make_float2(kNoScore, 0.f);
-    if (lane < n) ml = mine < n_own ? ml_own[(int64_t)mine * a.n_q_heads] : ml_shared[(int64_t)(mine - n_own) * kSharedTileRows];
-    float m_new = ml.x;
+    for (int e = 0; e < E; ++e) oo[e] = 0.f;
+    const int n_all = cut.z;
+    const int64_t first = 2 * (int64_t)piece;
+    auto slot = [&](int part) { return (first + (part == 0 ? 1 : 2 * part)) * a.group + h; };
+    for (int base = warp; base < n_all; base += 32 * kWarps) {  // 32 parts at a time: one (m, l) per lane
+      const int n = min(32, (n_all - base + kWarps - 1) / kWarps), mine = base + lane * kWarps;
+      float2 ml = make_float2(kNoScore, 0.f);
+      if (lane < n) ml = a.part_ml[slot(mine)];
+      float m_new = ml.x;
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) m_new = fmaxf(m_new, __shfl_xor_sync(0xffffffffu, m_new, o));
-    m_new = fmaxf(mm, m_new);
-    const float alpha = ex2(mm - m_new), f = ex2(ml.x - m_new);
-    mm = m_new;
-    float l = ml.y * f;
+      for (int o = 16; o > 0; o >>= 1) m_new = fmaxf(m_new, __shfl_xor_sync(0xffffffffu, m_new, o));
+      m_new = fmaxf(mm, m_new);
+      const float alpha = ex2(mm - m_new), f = ex2(ml.x - m_new);
+      mm = m_new;
+      float l = ml.y * f;
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
-    ll = ll * alpha + l;
+      for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+      ll = ll * alpha + l;
 #pragma unroll
-    for (int e = 0; e < E; ++e) oo[e] *= alpha;
+      for (int e = 0; e < E; ++e) oo[e] *= alpha;
 #pragma unroll 8
-    for (int c = 0; c < n; ++c) {
-      const float fc = __shfl_sync(0xffffffffu, f, c);
-      const int part = base + c * step;
-      const float* src = (part < n_own ? o_own + (int64_t)part * a.n_q_heads * D : o_shared + (int64_t)(part - n_own) * kSharedTileRows * D) + E * lane;
-      float p[E];
-      if constexpr (E == 4) {
-        const float4 x = *reinterpret_cast<const float4*>(src);
-        p[0] = x.x; p[1] = x.y; p[2] = x.z; p[3] = x.w;
-      } else {
-        const float2 x = *reinterpret_cast<const float2*>(src);
-        p[0] = x.x; p[1] = x.y;
-      }
+      for (int c = 0; c < n; ++c) {
+        const float fc = __shfl_sync(0xffffffffu, f, c);
+        const float* src = a.part_o + slot(base + c * kWarps) * D + E * lane;
+        float p[E];
+        if constexpr (E == 4) {
+          const float4 x = *reinterpret_cast<const float4*>(src);
+          p[0] = x.x; p[1] = x.y; p[2] = x.z; p[3] = x.w;
+        } else {
+          const float2 x = *reinterpret_cast<const float2*>(src);
+          p[0] = x.x; p[1] = x.y;
+        }
 #pragma unroll
-      for (int e = 0; e < E; ++e) oo[e] += p[e] * fc;
+        for (int e = 0; e < E; ++e) oo[e] += p[e] * fc;
+      }
     }
-  }
-  if constexpr (kAcross) {
     if (lane == 0) { s_m[warp] = mm; s_l[warp] = ll; }
 #pragma unroll
     for (int e = 0; e < E; ++e) s_o[warp][E * lane + e] = oo[e];
     __syncthreads();
-    if (warp != 0) return;
-    mm = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3]));
-    ll = 0.f;
+    if (threadIdx.x < D) {
+      mm = s_m[0];
 #pragma unroll
-    for (int e = 0; e < E; ++e) oo[e] = 0.f;
+      for (int w = 1; w < kWarps; ++w) mm = fmaxf(mm, s_m[w]);
+      ll = 0.f;
+      float o = 0.f;
 #pragma unroll
-    for (int w = 0; w < kPagedWarps; ++w) {
-      const float f = ex2(s_m[w] - mm);
-      ll += s_l[w] * f;
-#pragma unroll
-      for (int e = 0; e < E; ++e) oo[e] += s_o[w][E * lane + e] * f;
+      for (int w = 0; w < kWarps; ++w) {
+        const float f = ex2(s_m[w] - mm);
+        ll += s_l[w] * f;
+        o += s_o[w][threadIdx.x] * f;
+      }
+      // (an item that is cut has rows)
+      a.o[((int64_t)cut.x * a.n_q_heads + cut.y * a.group + h) * D + threadIdx.x] = __float2bfloat16_rn(o / ll);
     }
+    __syncthreads();
   }
-  uint32_t r[E / 2];
-  const bool none = len + (int)fresh <= 0;
-#pragma unroll
-  for (int e = 0; e < E / 2; ++e) r[e] = none ? 0u : round_bf16(oo[2 * e] / ll, oo[2 * e + 1] / ll);
-  __nv_bfloat16* dst = a.o + ((int64_t)i * a.n_q_heads + head) * D + E * lane;
-  if constexpr (E == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(r[0], r[1]);
-  else *reinterpret_cast<uint32_t*>(dst) = r[0];
 }
 
 // ------------------------------------------------------------------------------------------
@@ -916,7 +1152,7 @@ shared_plan_kernel(const __grid_constant__ PlanArgs p) {
     const int tiles = (rows + kSharedTileKeys - 1) / kSharedTileKeys;
     units += (int64_t)tiles * ((prompts * a.group + kSharedTileRows - 1) / kSharedTileRows) * a.n_kv_heads;
   }
-  int64_t at = block_prefix<kPlanThreads>(units, s_warp);
+  int64_t all, at = block_prefix<kPlanThreads>(units, s_warp, all);
   for (int g = g0; g < g1; ++g) {
     const int prompts = bad ? 0 : s_ptr[g + 1] - s_ptr[g], tiles = (s_rows[g] + kSharedTileKeys - 1) / kSharedTileKeys;
     plan.unit_start[g] = at;
@@ -925,15 +1161,65 @@ shared_plan_kernel(const __grid_constant__ PlanArgs p) {
     plan.lead[g] = s_lead[g];
     at += (int64_t)tiles * ((prompts * a.group + kSharedTileRows - 1) / kSharedTileRows) * a.n_kv_heads;
   }
-  if (tid == kPlanThreads - 1) {        // (the last thread's share ends the line, also where it is empty)
-    plan.unit_start[n] = at;
-    *plan.units = at;
+  if (tid == 0) {
+    plan.unit_start[n] = all;
+    *plan.units = all;
   }
   __syncthreads();
   for (int i = tid; i < k; i += kPlanThreads) {
     const int g = group_of(i);
     plan.own_start[i] = g >= 0 && a.lengths[i] >= 0 ? s_rows[g] : 0;
   }
+}
+
+// The parts of every query head over the shared rows, from the CTAs of the attention kernel, become one: a warp for each head of
+// each prompt. The step over the prompts' own rows goes on from there.
+template <int D>
+__global__ void __launch_bounds__(kCombineThreads)
+shared_join_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ SharedPlan plan) {
+  constexpr int E = D / 32;
+  const int lane = threadIdx.x & 31;
+  const int64_t row = (int64_t)blockIdx.x * (kCombineThreads / 32) + (threadIdx.x >> 5);
+  pdl_wait();
+  pdl_launch_dependents();
+  if (row >= (int64_t)a.n_prompts * a.n_q_heads) return;
+  const int i = (int)(row / a.n_q_heads), head = (int)(row - (int64_t)i * a.n_q_heads), kvh = head / a.group;
+  if (plan.own_start[i] == 0) return;   // nothing shared
+  const int gr = plan.group_of[i], tiles = plan.key_tiles[gr], first = plan.group_ptr[gr], rows = (plan.group_ptr[gr + 1] - first) * a.group;
+  const int r = (i - first) * a.group + head - kvh * a.group, rt = r / kSharedTileRows;
+  const int64_t per = units_per_piece(*plan.units, plan.n_ctas);
+  const int64_t u0 = plan.unit_start[gr] + ((int64_t)kvh * ((rows + kSharedTileRows - 1) / kSharedTileRows) + rt) * tiles;
+  const int p0 = (int)(u0 / per), n = (int)((u0 + tiles - 1) / per) - p0 + 1;
+  const int64_t at = (int64_t)p0 * kSharedTileRows + (int64_t)(first - plan.group_ptr[0]) * a.n_kv_heads * a.group + (int64_t)kvh * rows + r;
+  float mm = kNoScore, ll = 0.f, oo[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) oo[e] = 0.f;
+  for (int base = 0; base < n; base += 32) {
+    const int here = min(32, n - base);
+    const float2 ml = lane < here ? plan.ml[at + (int64_t)(base + lane) * kSharedTileRows] : make_float2(kNoScore, 0.f);
+    float m_new = ml.x;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m_new = fmaxf(m_new, __shfl_xor_sync(0xffffffffu, m_new, o));
+    m_new = fmaxf(mm, m_new);
+    const float alpha = ex2(mm - m_new), f = ex2(ml.x - m_new);
+    mm = m_new;
+    float l = ml.y * f;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+    ll = ll * alpha + l;
+#pragma unroll
+    for (int e = 0; e < E; ++e) oo[e] *= alpha;
+#pragma unroll 8
+    for (int c = 0; c < here; ++c) {
+      const float fc = __shfl_sync(0xffffffffu, f, c);
+      const float* src = plan.o + (at + (int64_t)(base + c) * kSharedTileRows) * D + E * lane;
+#pragma unroll
+      for (int e = 0; e < E; ++e) oo[e] += src[e] * fc;
+    }
+  }
+  if (lane == 0) plan.row_ml[row] = make_float2(mm, ll);
+#pragma unroll
+  for (int e = 0; e < E; ++e) plan.row_o[row * D + E * lane + e] = oo[e];
 }
 
 // ------------------------------------------------------------------------------------------
@@ -993,18 +1279,35 @@ int row_stride(int64_t given, int64_t dense, int64_t* out) {
   return *out % 8 ? PP_ERR_ALIGNMENT : PP_OK;
 }
 
+// 5-D map (column, row, chunk of 128 bytes, head, page) over a pool of pages; box = 16 rows of one head.
+bool page_map(CUtensorMap* map, const void* pages, const PagedArgs& a, int d, bool e4m3) {
+  EncodeFn enc = get_encode_fn();
+  if (!enc) return false;
+  const int size = e4m3 ? 1 : 2, columns = std::min(d, 128 / size);
+  const cuuint64_t dims[5] = {(cuuint64_t)columns, (cuuint64_t)1 << a.c.page_shift, (cuuint64_t)(d / columns), (cuuint64_t)a.n_kv_heads, (cuuint64_t)a.c.n_pages};
+  const cuuint64_t strides[4] = {(cuuint64_t)a.c.row_stride, 128u, (cuuint64_t)a.c.head_stride, (cuuint64_t)a.c.page_stride};
+  const cuuint32_t box[5] = {(cuuint32_t)columns, 16u, (cuuint32_t)(d / columns), 1u, 1u}, ones[5] = {1u, 1u, 1u, 1u, 1u};
+  return enc(map, e4m3 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void*>(pages), dims, strides, box, ones,
+             CU_TENSOR_MAP_INTERLEAVE_NONE, columns * size == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <int D, bool kE4m3>
-cudaError_t launch_paged_decode(const PagedArgs& a, int grid, size_t smem, cudaStream_t s) {
+cudaError_t launch_paged_decode(const PagedArgs& a, const SharedPlan& plan, cudaStream_t s) {
   static DeviceOnce configured;
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   if (!configured.done(dev)) {
-    e = cudaFuncSetAttribute(paged_decode_kernel<D, kE4m3>, cudaFuncAttributeMaxDynamicSharedMemorySize, (kMaxPagedPrompts + 1) * (int)sizeof(int32_t));
+    e = cudaFuncSetAttribute(paged_decode_kernel<D, kE4m3>, cudaFuncAttributeMaxDynamicSharedMemorySize, kStepSmem);
     if (e != cudaSuccess) return e;
     configured.mark(dev);
   }
-  return launch_dependent(paged_decode_kernel<D, kE4m3>, dim3(grid), dim3(kPagedThreads), smem, s, a);
+  CUtensorMap mk, mv;
+  if (!page_map(&mk, a.c.k_pages, a, D, kE4m3) || !page_map(&mv, a.c.v_pages, a, D, kE4m3)) return cudaErrorInvalidValue;
+  e = launch_dependent(paged_decode_kernel<D, kE4m3>, dim3(kSms), dim3(kStepThreads), (size_t)kStepSmem, s, mk, mv, a, plan);
+  if (e != cudaSuccess) return e;
+  return launch_dependent(paged_combine_kernel<D>, dim3(kCombineBlocks, a.group), dim3(kCombineThreads), 0, s, a);
 }
 
 template <int D>
@@ -1052,17 +1355,17 @@ int decode_step(const pp_attn_params* params, const pp_paged_cache* cache, const
   a.k_new = static_cast<const __nv_bfloat16*>(k_new);
   a.v_new = static_cast<const __nv_bfloat16*>(v_new);
   a.o = static_cast<__nv_bfloat16*>(o);
-  a.chunk_ptr = reinterpret_cast<int32_t*>(ws + L.chunk_ptr);
+  a.cut = reinterpret_cast<int4*>(ws + L.cut);
   a.part_ml = reinterpret_cast<float2*>(ws + L.part_ml);
   a.part_o = reinterpret_cast<float*>(ws + L.part_o);
   a.n_prompts = k;
   a.n_q_heads = params->n_q_heads;
   a.n_kv_heads = params->n_kv_heads;
   a.group = params->n_q_heads / params->n_kv_heads;
-  a.chunks_wanted = L.chunks_wanted;
   const float scale = params->softmax_scale > 0.f ? params->softmax_scale : 1.0f / sqrtf((float)params->head_dim);
   a.scale_log2 = scale * 1.4426950408889634f;
   a.status = device_status;
+  a.wait_limit = (uint32_t)std::min<unsigned long long>(wait_limit_ns() >> 10, 0x7fffffffu);
   a.angles = rope_angles(params->rope_base, params->head_dim);
   SharedPlan plan = {};
   if (n_groups > 0) {
@@ -1076,6 +1379,8 @@ int decode_step(const pp_attn_params* params, const pp_paged_cache* cache, const
     plan.q_rot = reinterpret_cast<__nv_bfloat16*>(ws + L.q_rot);
     plan.ml = reinterpret_cast<float2*>(ws + L.shared_ml);
     plan.o = reinterpret_cast<float*>(ws + L.shared_o);
+    plan.row_ml = reinterpret_cast<float2*>(ws + L.row_ml);
+    plan.row_o = reinterpret_cast<float*>(ws + L.row_o);
     plan.group_ptr = group_ptr;
     plan.n_groups = n_groups;
     plan.n_ctas = kSms;
@@ -1083,28 +1388,15 @@ int decode_step(const pp_attn_params* params, const pp_paged_cache* cache, const
     const cudaError_t e = d == 128 ? launch_plan<128>(p, s) : launch_plan<64>(p, s);
     if (e != cudaSuccess) return note_cuda_error((int)e, "plan kernel launch");
     if ((st = launch_shared_attention(*params, a.c, plan, k, a.scale_log2, device_status, s)) != PP_OK) return st;
+    const dim3 rows((unsigned)(((int64_t)k * params->n_q_heads + kCombineThreads / 32 - 1) / (kCombineThreads / 32)));
+    const cudaError_t joined = d == 128 ? launch_dependent(shared_join_kernel<128>, rows, dim3(kCombineThreads), 0, s, a, plan)
+                                        : launch_dependent(shared_join_kernel<64>, rows, dim3(kCombineThreads), 0, s, a, plan);
+    if (joined != cudaSuccess) return note_cuda_error((int)joined, "join kernel launch");
   }
-  // three CTAs per SM (four at D = 64), or as many as there can be chunks
-  const int64_t most_blocks = std::max<int64_t>(((int64_t)cache->table_stride * cache->page_size + kBlockKeys - 1) / kBlockKeys, 1);
-  const int64_t most = std::min<int64_t>((int64_t)k * most_blocks, (int64_t)L.chunks_wanted + k) * params->n_kv_heads;
-  const int grid = (int)std::min<int64_t>(most, kSms * (d == 128 ? 3 : 4));
-  const size_t smem = ((size_t)k + 1) * sizeof(int32_t);
   const bool e4m3 = cache->type == PP_CACHE_E4M3;
-  cudaError_t e = d == 128 ? (e4m3 ? launch_paged_decode<128, true>(a, grid, smem, s) : launch_paged_decode<128, false>(a, grid, smem, s))
-                           : (e4m3 ? launch_paged_decode<64, true>(a, grid, smem, s) : launch_paged_decode<64, false>(a, grid, smem, s));
-  if (e != cudaSuccess) return note_cuda_error((int)e, "paged generation step launch");
-  if (n_groups == 0 && most_blocks == 1) return PP_OK;         // no prompt can have two chunks
-  // four warps for a head as long as all of them run at once
-  if ((int64_t)k * params->n_q_heads <= kSms * 16) {
-    const dim3 heads((unsigned)k, (unsigned)params->n_q_heads);
-    e = d == 128 ? launch_dependent(paged_combine_kernel<128, true>, heads, dim3(kPagedThreads), 0, s, a, plan)
-                 : launch_dependent(paged_combine_kernel<64, true>, heads, dim3(kPagedThreads), 0, s, a, plan);
-  } else {
-    const dim3 heads((unsigned)k, (unsigned)((params->n_q_heads + kPagedWarps - 1) / kPagedWarps));
-    e = d == 128 ? launch_dependent(paged_combine_kernel<128, false>, heads, dim3(kPagedThreads), 0, s, a, plan)
-                 : launch_dependent(paged_combine_kernel<64, false>, heads, dim3(kPagedThreads), 0, s, a, plan);
-  }
-  return e == cudaSuccess ? PP_OK : note_cuda_error((int)e, "paged combine launch");
+  const cudaError_t e = d == 128 ? (e4m3 ? launch_paged_decode<128, true>(a, plan, s) : launch_paged_decode<128, false>(a, plan, s))
+                                 : (e4m3 ? launch_paged_decode<64, true>(a, plan, s) : launch_paged_decode<64, false>(a, plan, s));
+  return e == cudaSuccess ? PP_OK : note_cuda_error((int)e, "paged generation step launch");
 }
 
 }  // namespace
@@ -1123,9 +1415,8 @@ PagedWorkspace paged_workspace(const pp_attn_params& p, int32_t k, int32_t n_gro
     at = (at + bytes + 255) & ~size_t(255);
     return here;
   };
-  L.chunks_wanted = std::max(kChunksWanted / p.n_kv_heads, 1);
-  const size_t parts = ((size_t)L.chunks_wanted + k) * p.n_q_heads;
-  L.chunk_ptr = take(((size_t)k + 1) * sizeof(int32_t));
+  const size_t parts = 2 * (size_t)kPieces * (p.n_q_heads / p.n_kv_heads);
+  L.cut = take((size_t)kPieces * sizeof(int4));
   L.part_ml = take(parts * sizeof(float2));
   L.part_o = take(parts * p.head_dim * sizeof(float));
   if (n_groups > 0) {
@@ -1140,6 +1431,8 @@ PagedWorkspace paged_workspace(const pp_attn_params& p, int32_t k, int32_t n_gro
     const size_t rows = (size_t)kSms * kSharedTileRows + (size_t)k * p.n_q_heads;
     L.shared_ml = take(rows * sizeof(float2));
     L.shared_o = take(rows * p.head_dim * sizeof(float));
+    L.row_ml = take((size_t)k * p.n_q_heads * sizeof(float2));
+    L.row_o = take((size_t)k * p.n_q_heads * p.head_dim * sizeof(float));
   }
   L.total = at;
   return L;

@@ -47,13 +47,13 @@ struct RopeAngles {
 };
 RopeAngles rope_angles(float base, int32_t head_dim);
 
-// Partial results of a step: (m, l), m in scaled log2 units, and the unnormalised sum of D floats for each (part, query head).
-// Own rows: part = chunk of a prompt. Shared rows (kernel over kSharedTileRows x kSharedTileKeys tiles): the work is a line of
+// Parts of results: (m, l), m in scaled log2 units, and the unnormalised sum of D floats for a query head.
+// Own rows: pp_paged.cu. Shared rows (a kernel over kSharedTileRows x kSharedTileKeys tiles): the work is a line of
 // units, one tile of keys against one tile of rows each, ordered by (group, KV head, row tile, key tile), and cut into equal
 // pieces, one for each CTA. CTA c's part of an item (group, KV head, row tile) lies at rows c * kSharedTileRows + (rows of all
 // items before it) of the arrays: pieces and items both only ascend, and an item has at most kSharedTileRows rows.
 struct PagedWorkspace {
-  size_t chunk_ptr;                     // int32 [k + 1]
+  size_t cut;                           // int4 for each piece of the line of own rows
   size_t part_ml, part_o;               // float2, float[D]
   // with shared rows only
   size_t units;                         // int64: units in all
@@ -64,9 +64,9 @@ struct PagedWorkspace {
   size_t own_start;                     // int32 [k]: first row that the prompt reads on its own
   size_t group_of;                      // int32 [k], -1: none
   size_t q_rot;                         // bf16 [Hkv][k * group][D]
-  size_t shared_ml, shared_o;           // float2, float[D]
+  size_t shared_ml, shared_o;           // float2, float[D]: parts
+  size_t row_ml, row_o;                 // [k][Hq]: joined
   size_t total;
-  int32_t chunks_wanted;
 };
 PagedWorkspace paged_workspace(const pp_attn_params& p, int32_t k, int32_t n_groups);
 
@@ -76,8 +76,8 @@ struct SharedPlan {
   int64_t* unit_start;
   int32_t *key_tiles, *shared_rows, *lead, *own_start, *group_of;
   __nv_bfloat16* q_rot;
-  float2* ml;
-  float* o;
+  float2 *ml, *row_ml;
+  float *o, *row_o;
   const int32_t* group_ptr;
   int32_t n_groups, n_ctas;             // n_ctas: pieces that the line of units is cut into
 };

@@ -119,9 +119,10 @@ def attend64(q, keys, values, scale):
 def step_bound(o, size, big, n, d):
     """How far a step's O may be off. A query reaches the products in two 16-bit parts (2^-16 of it is lost) after a rotation in
     fp32 (3 roundings), a score is a sum of 2 d products in fp32 (2 d 2^-24 of the sum of magnitudes, twice that for
-    tensor cores that truncate), its exponential has 2^-22: a score that is off by e moves O by at most 2 e max|v|. Sums of n
+    tensor cores that truncate), its exponential has 2^-22, and a weight too reaches the products in two 16-bit parts (2^-16): a score
+    or the logarithm of a weight that is off by e moves O by at most 2 e max|v|. Sums of n
     weights and products in fp32: n 2^-23 max|v|. The last rounding: 2^-8 of O (half of a step of bf16)."""
-    e = size * (2.0 ** -16 + (4 * d + 8) * 2.0 ** -24) + 2.0 ** -22
+    e = size * (2.0 ** -16 + (4 * d + 8) * 2.0 ** -24) + 2.0 ** -16 + 2.0 ** -22
     return np.abs(o) * 2.0 ** -8 + ((2 * e + (n + 64) * 2.0 ** -23) * big)[:, None] + 1e-30
 
 
