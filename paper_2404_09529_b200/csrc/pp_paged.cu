@@ -211,8 +211,8 @@ append_kernel(const __grid_constant__ AppendArgs a) {
 // way. A piece that is a whole item (prompt, KV head) leaves O at once; of an item that is cut the parts (m, l, o) are joined by
 // paged_combine_kernel.
 // The arithmetic is that of the step over contiguous caches (pp_decode.cu): mma.m16n8k16 with 16 keys as rows and the query heads
-// of a KV head as the 8 columns, absent heads 0. A query and a weight each reach it as the sum of two 16-bit numbers: HBM
-// leaves the tensor cores idle, and scores and O are then exact to 2^-16, far below O's last rounding of 2^-8.
+// of a KV head as the 8 columns, absent heads 0. Over bf16 pages a query and a weight each reach it as the sum of two
+// 16-bit numbers: HBM leaves the tensor cores idle, and scores and O are then exact to 2^-16, far below O's last rounding of 2^-8.
 // The lengths live on the device: every CTA sums them itself, and the grid and the room for parts depend on neither them nor k.
 constexpr int kMaxGroup = 8;            // query heads per KV head: the N of the tensor-core product
 constexpr int kStepWarps = 12, kStepThreads = 32 * kStepWarps;
@@ -329,6 +329,7 @@ template <int D>
 struct Rows<D, false> {
   static constexpr int kRowBytes = 2 * D, kSteps = kHalfUnit / (16 * kRowBytes);      // steps of 16 keys in a unit
   static constexpr float kWeight = 1.f;
+  static constexpr bool kLowPart = true;
   // A step's box, as TMA leaves it: chunks of 64 elements one behind the other, rows of 128 bytes, the 16-byte pieces of 8 rows
   // swizzled so that one of each row fill all banks once.
   static constexpr int kStepBytes = 16 * kRowBytes, kChunkBytes = 2048;
@@ -443,8 +444,10 @@ struct Rows<D, false> {
 template <int D>
 struct Rows<D, true> {
   static constexpr int kRowBytes = D, kSteps = kHalfUnit / (16 * kRowBytes);
-  // Weights are at most 2^kLazyLog2 and multiplied in two f16 parts, which end at 2^-24: times 2^11 they reach down to 2^-35 of
-  // the largest, so that what the sum of 2^17 of the smallest loses is still below 2^-18 of it.
+  // Queries and weights are rounded to f16 once: 11 bits, 2^-12 of each, against the 2^-8 of O's last rounding and keys of 4 bits.
+  // Weights are at most 2^kLazyLog2; times 2^11 those down to 2^-25 of the largest have all of their bits, and what the sum of 2^17
+  // of the smallest loses is below 2^-18 of it.
+  static constexpr bool kLowPart = false;
   static constexpr float kWeight = 2048.f;
   // A step's box, as TMA leaves it: rows of 128 (64) bytes, whose 16-byte pieces are swizzled.
   static constexpr int kStepBytes = 16 * kRowBytes;
@@ -457,24 +460,22 @@ struct Rows<D, true> {
       q[4 * i] = x.x; q[4 * i + 1] = x.y; q[4 * i + 2] = x.z; q[4 * i + 3] = x.w;
     }
   }
-  static __device__ __forceinline__ void mma_scores(float (&c)[4], const uint4 (&r0)[D / 64], const uint4 (&r1)[D / 64], const uint32_t (&qh)[D / 8],
-                                                    const uint32_t (&ql)[D / 8]) {
-    float p[4][4];
+  static __device__ __forceinline__ void mma_scores(float (&c)[4], const uint4 (&r0)[D / 64], const uint4 (&r1)[D / 64], const uint32_t (&q)[D / 8]) {
+    float p[2][4];
 #pragma unroll
-    for (int x = 0; x < 4; ++x) p[x][0] = p[x][1] = p[x][2] = p[x][3] = 0.f;
+    for (int x = 0; x < 2; ++x) p[x][0] = p[x][1] = p[x][2] = p[x][3] = 0.f;
 #pragma unroll
     for (int i = 0; i < D / 64; ++i)
 #pragma unroll
       for (int w = 0; w < 4; ++w) {                   // four elements of a row in each word of the piece
         const uint32_t x0 = word_of(r0[i], w), x1 = word_of(r1[i], w);
         const uint32_t a0 = f16_of_e4m3_lo(x0), a1 = f16_of_e4m3_lo(x1), a2 = f16_of_e4m3_hi(x0), a3 = f16_of_e4m3_hi(x1);
-        mma16816_f16(p[w & 1], a0, a1, a2, a3, qh[8 * i + 2 * w], qh[8 * i + 2 * w + 1]);
-        mma16816_f16(p[2 + (w & 1)], a0, a1, a2, a3, ql[8 * i + 2 * w], ql[8 * i + 2 * w + 1]);
+        mma16816_f16(p[w & 1], a0, a1, a2, a3, q[8 * i + 2 * w], q[8 * i + 2 * w + 1]);
       }
 #pragma unroll
-    for (int x = 0; x < 4; ++x) c[x] = (p[0][x] + p[1][x]) + (p[2][x] + p[3][x]);
+    for (int x = 0; x < 4; ++x) c[x] = p[0][x] + p[1][x];
   }
-  static __device__ __forceinline__ void scores(float (&c)[4], uint32_t at, const uint32_t (&qh)[D / 8], const uint32_t (&ql)[D / 8], int lane) {
+  static __device__ __forceinline__ void scores(float (&c)[4], uint32_t at, const uint32_t (&q)[D / 8], const uint32_t (&)[D / 8], int lane) {
     uint4 r0[D / 64], r1[D / 64];
     const int g = lane >> 2, t = lane & 3;
 #pragma unroll
@@ -482,9 +483,9 @@ struct Rows<D, true> {
       r0[i] = shared16(at + place(g, D / 64 * t + i));
       r1[i] = shared16(at + place(g + 8, D / 64 * t + i));
     }
-    mma_scores(c, r0, r1, qh, ql);
+    mma_scores(c, r0, r1, q);
   }
-  static __device__ __forceinline__ void scores_one(float (&c)[4], uint32_t at, const uint32_t (&qh)[D / 8], const uint32_t (&ql)[D / 8], int g, int t) {
+  static __device__ __forceinline__ void scores_one(float (&c)[4], uint32_t at, const uint32_t (&q)[D / 8], const uint32_t (&)[D / 8], int g, int t) {
     uint4 r0[D / 64], r1[D / 64];
     const uint4 none = make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
@@ -493,19 +494,15 @@ struct Rows<D, true> {
       r0[i] = g == 0 ? x : none;
       r1[i] = none;
     }
-    mma_scores(c, r0, r1, qh, ql);
+    mma_scores(c, r0, r1, q);
   }
-  struct Weights { uint32_t b[2][2]; };
+  struct Weights { uint32_t b[2]; };
   static __device__ __forceinline__ Weights weights(const float (&p)[4]) {
     Weights w;
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
-      const float p0 = p[2 * x] * kWeight, p1 = p[2 * x + 1] * kWeight;
-      const __half2 h = __floats2half2_rn(p0, p1);
-      const float2 back = __half22float2(h);
-      const __half2 l = __floats2half2_rn(p0 - back.x, p1 - back.y);
-      w.b[0][x] = transpose8x8(*reinterpret_cast<const uint32_t*>(&h));
-      w.b[1][x] = transpose8x8(*reinterpret_cast<const uint32_t*>(&l));
+      const __half2 h = __floats2half2_rn(p[2 * x] * kWeight, p[2 * x + 1] * kWeight);
+      w.b[x] = transpose8x8(*reinterpret_cast<const uint32_t*>(&h));
     }
     return w;
   }
@@ -515,8 +512,7 @@ struct Rows<D, true> {
     for (int y = 0; y < 2; ++y) {
       const uint32_t k0 = __byte_perm(r0, r1, y ? 0x7362 : 0x5140), k1 = __byte_perm(r2, r3, y ? 0x7362 : 0x5140);
       const uint32_t a0 = f16_of_e4m3_lo(k0), a1 = f16_of_e4m3_hi(k0), a2 = f16_of_e4m3_lo(k1), a3 = f16_of_e4m3_hi(k1);
-      mma16816_f16(acc[2 * w + y], a0, a1, a2, a3, p.b[1][0], p.b[1][1]);
-      mma16816_f16(acc[2 * w + y], a0, a1, a2, a3, p.b[0][0], p.b[0][1]);
+      mma16816_f16(acc[2 * w + y], a0, a1, a2, a3, p.b[0], p.b[1]);
     }
   }
   static __device__ __forceinline__ void product(float (&acc)[D / 16][4], uint32_t at, const float (&p)[4], int lane) {
@@ -559,11 +555,7 @@ struct Rows<D, true> {
     const __half2 h = __floats2half2_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&h);
   }
-  static __device__ __forceinline__ uint32_t low(float a, float b, uint32_t h) {
-    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
-    const __half2 l = __floats2half2_rn(isfinite(f.x) ? a - f.x : 0.f, isfinite(f.y) ? b - f.y : 0.f);
-    return *reinterpret_cast<const uint32_t*>(&l);
-  }
+  static __device__ __forceinline__ uint32_t low(float, float, uint32_t) { return 0u; }
 };
 
 // A warp's place on the line: the part of an item (prompt i, KV head kvh) that lies in its piece. An item takes kItemUnits of the line
@@ -832,16 +824,18 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
     __syncwarp();
     R::load_q(qh, scratch + g * kQPitch, t);
     __syncwarp();
+    if constexpr (R::kLowPart) {
 #pragma unroll
-    for (int x = 0; x < kMaxGroup / kHeadsAtOnce; ++x) {
-      if (x * kHeadsAtOnce >= a.group) break;
-      const int h = x * kHeadsAtOnce + lane / kLanesPerHead;
-      *reinterpret_cast<uint2*>(scratch_p + h * kQPitch + 2 * j0) = lo2[x];
-      *reinterpret_cast<uint2*>(scratch_p + h * kQPitch + 2 * (j0 + kHalf)) = hi2[x];
+      for (int x = 0; x < kMaxGroup / kHeadsAtOnce; ++x) {
+        if (x * kHeadsAtOnce >= a.group) break;
+        const int h = x * kHeadsAtOnce + lane / kLanesPerHead;
+        *reinterpret_cast<uint2*>(scratch_p + h * kQPitch + 2 * j0) = lo2[x];
+        *reinterpret_cast<uint2*>(scratch_p + h * kQPitch + 2 * (j0 + kHalf)) = hi2[x];
+      }
+      __syncwarp();
+      R::load_q(ql, scratch + g * kQPitch, t);
+      __syncwarp();
     }
-    __syncwarp();
-    R::load_q(ql, scratch + g * kQPitch, t);
-    __syncwarp();
     if (g >= a.group) {                 // absent heads
 #pragma unroll
       for (int x = 0; x < D / 8; ++x) qh[x] = ql[x] = 0u;
@@ -1004,36 +998,41 @@ paged_combine_kernel(const __grid_constant__ PagedArgs a) {
     const int n_all = cut.z;
     const int64_t first = 2 * (int64_t)piece;
     auto slot = [&](int part) { return (first + (part == 0 ? 1 : 2 * part)) * a.group + h; };
-    for (int base = warp; base < n_all; base += 32 * kWarps) {  // 32 parts at a time: one (m, l) per lane
-      const int n = min(32, (n_all - base + kWarps - 1) / kWarps), mine = base + lane * kWarps;
-      float2 ml = make_float2(kNoScore, 0.f);
-      if (lane < n) ml = a.part_ml[slot(mine)];
-      float m_new = ml.x;
+    constexpr int kAtOnce = 4;          // parts whose loads are under way together
+    for (int base = warp; base < n_all; base += kAtOnce * kWarps) {
+      float2 ml[kAtOnce];
+      float p[kAtOnce][E];
 #pragma unroll
-      for (int o = 16; o > 0; o >>= 1) m_new = fmaxf(m_new, __shfl_xor_sync(0xffffffffu, m_new, o));
-      m_new = fmaxf(mm, m_new);
-      const float alpha = ex2(mm - m_new), f = ex2(ml.x - m_new);
-      mm = m_new;
-      float l = ml.y * f;
+      for (int c = 0; c < kAtOnce; ++c) {
+        ml[c] = make_float2(kNoScore, 0.f);
 #pragma unroll
-      for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
-      ll = ll * alpha + l;
-#pragma unroll
-      for (int e = 0; e < E; ++e) oo[e] *= alpha;
-#pragma unroll 8
-      for (int c = 0; c < n; ++c) {
-        const float fc = __shfl_sync(0xffffffffu, f, c);
-        const float* src = a.part_o + slot(base + c * kWarps) * D + E * lane;
-        float p[E];
+        for (int e = 0; e < E; ++e) p[c][e] = 0.f;
+        if (base + c * kWarps >= n_all) continue;
+        const int64_t at = slot(base + c * kWarps);
+        ml[c] = a.part_ml[at];
+        const float* src = a.part_o + at * D + E * lane;
         if constexpr (E == 4) {
           const float4 x = *reinterpret_cast<const float4*>(src);
-          p[0] = x.x; p[1] = x.y; p[2] = x.z; p[3] = x.w;
+          p[c][0] = x.x; p[c][1] = x.y; p[c][2] = x.z; p[c][3] = x.w;
         } else {
           const float2 x = *reinterpret_cast<const float2*>(src);
-          p[0] = x.x; p[1] = x.y;
+          p[c][0] = x.x; p[c][1] = x.y;
         }
+      }
+      float m_new = mm;
 #pragma unroll
-        for (int e = 0; e < E; ++e) oo[e] += p[e] * fc;
+      for (int c = 0; c < kAtOnce; ++c) m_new = fmaxf(m_new, ml[c].x);
+      const float alpha = ex2(mm - m_new);
+      mm = m_new;
+      ll *= alpha;
+#pragma unroll
+      for (int e = 0; e < E; ++e) oo[e] *= alpha;
+#pragma unroll
+      for (int c = 0; c < kAtOnce; ++c) {
+        const float f = ex2(ml[c].x - m_new);
+        ll += ml[c].y * f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) oo[e] += p[c][e] * f;
       }
     }
     if (lane == 0) { s_m[warp] = mm; s_l[warp] = ll; }

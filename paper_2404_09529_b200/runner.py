@@ -279,7 +279,7 @@ class PagedCaches:
                 raise ValueError("8-bit pages, and only they, have scales")
             if e4m3 and (scale.dtype != torch.float32 or scale.shape != (self.hkv,) or scale.device != k_pages.device or not scale.is_contiguous()):
                 raise ValueError("a scale is a contiguous float32 [Hkv] tensor on the pools' device")
-        self.device, self.rows_first = k_pages.device, rows_first
+        self.device, self.index, self.rows_first = k_pages.device, k_pages.get_device(), rows_first
         self.k_pages, self.v_pages, self.page_table, self.k_scale, self.v_scale = k_pages, v_pages, page_table, k_scale, v_scale
         self.struct = B.PagedCache(
             k_pages.data_ptr(), v_pages.data_ptr(), k_scale.data_ptr() if e4m3 else None, v_scale.data_ptr() if e4m3 else None,
@@ -353,31 +353,40 @@ class PagedCaches:
         self._write_row(prompt)
 
     def check_new(self, x: torch.Tensor, rows: int, heads: int, what: str) -> int:
-        """The row stride of new rows [rows, heads, D]; slices of a fused projection are welcome."""
-        if x.dtype != torch.bfloat16 or x.device != self.device or tuple(x.shape) != (rows, heads, self.d):
+        """The row stride of new rows [rows, heads, D]; slices of a fused projection are welcome. (As few tensor attributes as
+        will do: each costs the host a tenth of a microsecond or more, and a step of a few prompts takes the GPU ten.)"""
+        if x.dtype is not torch.bfloat16 or x.get_device() != self.index or x.shape != (rows, heads, self.d):
             raise ValueError(f"{what}: a bfloat16 tensor of shape {(rows, heads, self.d)} on {self.device} is wanted")
-        if x.stride(2) != 1 or (heads > 1 and x.stride(1) != self.d):
+        s0, s1, s2 = x.stride()
+        if s2 != 1 or (s1 != self.d and heads > 1):
             raise ValueError(f"{what}: the heads of a row lie one behind the other")
-        if rows > 1 and x.stride(0) < heads * self.d:
+        if rows <= 1:
+            return 0
+        if s0 < heads * self.d:
             raise ValueError(f"{what}: every row has memory of its own")
-        return x.stride(0) if rows > 1 else 0
+        return s0
+
+    def check_ints(self, x: torch.Tensor, what: str) -> int:
+        """The length of a contiguous int32 vector on the pools' device."""
+        if x.dtype is not torch.int32 or x.dim() != 1 or x.get_device() != self.index or not x.is_contiguous():
+            raise ValueError(f"{what}: a contiguous int32 vector on the pools' device is wanted")
+        return x.shape[0]
 
     def append(self, prompt: torch.Tensor, position: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, rope_base: float,
                rotated: bool = False) -> None:
         """Row r of k_new, v_new [rows, Hkv, D] becomes row position[r] of prompt[r] (int32 tensors on the device; prompt < 0: no
         row), its key rotated by that position unless it is rotated already. On the current stream, asynchronous."""
-        rows = prompt.shape[0]
-        for x in (prompt, position):
-            if x.dtype != torch.int32 or x.shape != (rows,) or x.device != self.device or not x.is_contiguous():
-                raise ValueError("prompt and position are contiguous int32 tensors of one length on the pools' device")
-        strides = [self.check_new(x, rows, self.hkv, what) for x, what in ((k_new, "k_new"), (v_new, "v_new"))]
+        rows = self.check_ints(prompt, "prompt")
+        if self.check_ints(position, "position") != rows:
+            raise ValueError("prompt and position have one length")
+        k_stride, v_stride = self.check_new(k_new, rows, self.hkv, "k_new"), self.check_new(v_new, rows, self.hkv, "v_new")
         key = (rope_base, rotated)
         params = self._append_params.get(key)
         if params is None:
             params = B.AttnParams(self.hkv, self.hkv, self.d, rope_base, 0.0, 1, 1, B.PP_FLAG_SKIP_ROPE if rotated else 0)
             self._append_params[key] = params
         with on_device(self.device):
-            B.pp_paged_append(params, self.struct, prompt, position, rows, self.n_prompts, k_new, strides[0], v_new, strides[1],
+            B.pp_paged_append(params, self.struct, prompt, position, rows, self.n_prompts, k_new, k_stride, v_new, v_stride,
                               self.status, B.current_stream())
 
     def append_prefill(self, prefill: PrefillBatch) -> torch.Tensor:
@@ -424,15 +433,16 @@ class PagedDecoder:
         self._workspaces = []
         self._sizes = {}
 
-    def _workspace(self, k: int, n_groups: int) -> torch.Tensor:
+    def _workspace(self, k: int, n_groups: int):
+        """(workspace, its bytes) for these sizes."""
         need = self._sizes.get((k, n_groups))
         if need is None:
             need = B.pp_paged_decode_workspace_bytes(self.params, k, n_groups)
             if need == 0:
                 raise ValueError("no generation step for these shapes")
             self._sizes[(k, n_groups)] = need
-        if not self._workspaces or self._workspaces[-1].numel() < need:
-            self._workspaces.append(torch.empty(need, dtype=torch.uint8, device=self.caches.device))
+        if not self._workspaces or self._workspaces[-1][1] < need:
+            self._workspaces.append((torch.empty(need, dtype=torch.uint8, device=self.caches.device), need))
         return self._workspaces[-1]
 
     def step(self, lengths: torch.Tensor, q: torch.Tensor, k: torch.Tensor | None = None, v: torch.Tensor | None = None,
@@ -442,32 +452,33 @@ class PagedDecoder:
         shared_len), int32 on the device, where prompts share their first pages. Returns out [n, Hq, D]; on the
         current stream, asynchronous, nothing is read back. The lengths are the caller's to advance."""
         c = self.caches
-        n = lengths.shape[0]
-        if lengths.dtype != torch.int32 or lengths.dim() != 1 or lengths.device != c.device or not lengths.is_contiguous() or not 0 < n <= c.n_prompts:
-            raise ValueError("lengths: a contiguous int32 tensor on the pools' device, of at most the table's rows")
+        n = c.check_ints(lengths, "lengths")
+        if not 0 < n <= c.n_prompts:
+            raise ValueError("lengths: one for each of at most the table's rows")
         if (k is None) != (v is None):
             raise ValueError("a new token has a key and a value")
         q_stride = c.check_new(q, n, self.hq, "q")
-        k_stride, v_stride = (0, 0) if k is None else (c.check_new(k, n, c.hkv, "k"), c.check_new(v, n, c.hkv, "v"))
+        k_stride = v_stride = 0
+        if k is not None:
+            k_stride, v_stride = c.check_new(k, n, c.hkv, "k"), c.check_new(v, n, c.hkv, "v")
         if out is None:
             out = torch.zeros((n, self.hq, c.d), dtype=torch.bfloat16, device=c.device)
-        elif out.dtype != torch.bfloat16 or tuple(out.shape) != (n, self.hq, c.d) or out.device != c.device or not out.is_contiguous():
+        elif out.dtype is not torch.bfloat16 or out.shape != (n, self.hq, c.d) or out.get_device() != c.index or not out.is_contiguous():
             raise ValueError("out: a contiguous bfloat16 tensor of q's shape on the pools' device")
+        if groups is not None:
+            ptr, shared = groups
+            n_groups = c.check_ints(shared, "shared_len")
+            if c.check_ints(ptr, "group_ptr") != n_groups + 1:
+                raise ValueError("groups: group_ptr has one entry more than shared_len")
         with on_device(c.device):
             if groups is None:
-                ws = self._workspace(n, 0)
-                B.pp_paged_decode_step(self.params, c.struct, lengths, n, q, q_stride, k, k_stride, v, v_stride, out, ws, ws.numel(),
-                                       self.status, B.current_stream())
+                ws, size = self._workspace(n, 0)
+                B.pp_paged_decode_step(self.params, c.struct, lengths, n, q, q_stride, k, k_stride, v, v_stride, out, ws, size, self.status,
+                                       B.current_stream())
             else:
-                ptr, shared = groups
-                for x in (ptr, shared):
-                    if x.dtype != torch.int32 or x.dim() != 1 or x.device != c.device or not x.is_contiguous():
-                        raise ValueError("groups: contiguous int32 tensors on the pools' device")
-                if ptr.shape[0] != shared.shape[0] + 1:
-                    raise ValueError("groups: group_ptr has one entry more than shared_len")
-                ws = self._workspace(n, shared.shape[0])
-                B.pp_paged_decode_shared(self.params, c.struct, lengths, n, ptr, shared, shared.shape[0], q, q_stride, k, k_stride, v,
-                                         v_stride, out, ws, ws.numel(), self.status, B.current_stream())
+                ws, size = self._workspace(n, n_groups)
+                B.pp_paged_decode_shared(self.params, c.struct, lengths, n, ptr, shared, n_groups, q, q_stride, k, k_stride, v, v_stride, out,
+                                         ws, size, self.status, B.current_stream())
         return out
 
     def device_status(self) -> int:
