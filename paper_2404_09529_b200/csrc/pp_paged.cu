@@ -207,20 +207,19 @@ append_kernel(const __grid_constant__ AppendArgs a) {
 // Bound: HBM, every row of K and V is read once. The work is a line of units of 8 KB (16, 32 or 64 rows of K and V of one KV
 // head), ordered by (prompt, KV head, rows), and cut into equal pieces, one for each warp that the GPU holds: all warps read the
 // same number of bytes whatever the lengths are. A warp works on its own from there on. Its rows arrive by TMA in a ring of
-// two units in shared memory, whose loads run ahead over the ends of items, so that 12 warps keep up to 192 KB of an SM under
-// way. A piece that is a whole item (prompt, KV head) leaves O at once; of an item that is cut the parts (m, l, o) are joined by
+// two units in shared memory, whose loads run ahead over the ends of items. Six warps (seven over 8-bit pages, which take more
+// instructions a byte) keep up to 96 KB of an SM under way, which is all that HBM takes: with twelve, the loads queued up and SMs
+// were served so unevenly that of 148 equal shares the last ended 20 % after the mean. A piece that is a whole item (prompt, KV head) leaves O at once; of an item that is cut the parts (m, l, o) are joined by
 // paged_combine_kernel.
 // The arithmetic is that of the step over contiguous caches (pp_decode.cu): mma.m16n8k16 with 16 keys as rows and the query heads
 // of a KV head as the 8 columns, absent heads 0. Over bf16 pages a query and a weight each reach it as the sum of two
 // 16-bit numbers: HBM leaves the tensor cores idle, and scores and O are then exact to 2^-16, far below O's last rounding of 2^-8.
 // The lengths live on the device: every CTA sums them itself, and the grid and the room for parts depend on neither them nor k.
 constexpr int kMaxGroup = 8;            // query heads per KV head: the N of the tensor-core product
-constexpr int kStepWarps = 12, kStepThreads = 32 * kStepWarps;
-constexpr int kPieces = kSms * kStepWarps;
+constexpr int kMostStepWarps = 7, kMostPieces = kSms * kMostStepWarps;
 constexpr int kHalfUnit = 4096;         // bytes of K, and of V, in a unit
 constexpr int kScratch = 2304;          // per warp: queries, the new token's rows, O on its way out
-constexpr int kStepSmem = 1024 + kStepWarps * (4 * kHalfUnit + kScratch);    // rings on 1024-byte boundaries
-constexpr int kCombineThreads = 256, kCombineBlocks = 4 * kSms;
+constexpr int kCombineThreads = 256;
 // The running maximum of a row moves only when a score exceeds it by more than 2^kLazyLog2: until then no lane has to ask the
 // others (three exchanges for each of two heads). Sums are at most 2^kLazyLog2 as large, which costs fp32 nothing.
 constexpr float kLazyLog2 = 4.f;
@@ -233,9 +232,9 @@ struct PagedArgs {
   const __nv_bfloat16 *q_new, *k_new, *v_new;
   int64_t q_stride, k_stride, v_stride;
   __nv_bfloat16* o;
-  int4* cut;                            // [kPieces]: of the item that begins in a piece and ends in another: prompt, KV head, pieces; 0 pieces: none
-  float2* part_ml;                      // [2 kPieces][group]
-  float* part_o;                        // [2 kPieces][group][D]
+  int4* cut;                            // [pieces]: of the item that begins in a piece and ends in another: prompt, KV head, pieces; 0 pieces: none
+  float2* part_ml;                      // [2 pieces][group]
+  float* part_o;                        // [2 pieces][group][D]
   int32_t n_prompts, n_q_heads, n_kv_heads, group;
   float scale_log2;
   int32_t* status;
@@ -327,6 +326,7 @@ struct Rows;
 
 template <int D>
 struct Rows<D, false> {
+  static constexpr int kWarps = 6;
   static constexpr int kRowBytes = 2 * D, kSteps = kHalfUnit / (16 * kRowBytes);      // steps of 16 keys in a unit
   static constexpr float kWeight = 1.f;
   static constexpr bool kLowPart = true;
@@ -443,6 +443,7 @@ struct Rows<D, false> {
 // V rows 2t, 2t + 1, 2t + 8, 2t + 9, the g-th eighth of a row.
 template <int D>
 struct Rows<D, true> {
+  static constexpr int kWarps = 7;
   static constexpr int kRowBytes = D, kSteps = kHalfUnit / (16 * kRowBytes);
   // Queries and weights are rounded to f16 once: 11 bits, 2^-12 of each, against the 2^-8 of O's last rounding and keys of 4 bits.
   // Weights are at most 2^kLazyLog2; times 2^11 those down to 2^-25 of the largest have all of their bits, and what the sum of 2^17
@@ -559,8 +560,10 @@ struct Rows<D, true> {
 };
 
 // A warp's place on the line: the part of an item (prompt i, KV head kvh) that lies in its piece. An item takes kItemUnits of the line
-// more than it has units: the latencies at its beginning and end, in which its warp does not load.
-constexpr int kItemUnits = 1;
+// more than it has units: what its beginning and end cost its warp. With 1, 2, 3, 4 and 6 (seven warps; us a step): 256 prompts behind
+// 8192 shared rows -, 128, 124, 122, 122; 256 prompts of two lengths, 240 k rows, 32 / 8 heads -, 166, 168, 169, 168, in e4m3 -, 101, 92,
+// 94, 98; 64 prompts on 32 heads -, 55.8, 56.6, 57.8, 59.0.
+constexpr int kItemUnits = 3;
 struct Place {
   int64_t left;                         // of the piece, from here on
   int i, kvh;
@@ -617,17 +620,18 @@ struct Line {
 };
 
 template <int D, bool kE4m3>
-__global__ void __launch_bounds__(kStepThreads, 1)
+__global__ void __launch_bounds__(32 * Rows<D, kE4m3>::kWarps, 1)
 paged_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ PagedArgs a,
                     const __grid_constant__ SharedPlan plan) {
   using R = Rows<D, kE4m3>;
+  constexpr int kWarps = R::kWarps, kThreads = 32 * kWarps, kPieces = kSms * kWarps;
   constexpr int kSteps = R::kSteps, kUnitRows = 16 * kSteps, kHalf = D / 2, kSize = kE4m3 ? 1 : 2;
   constexpr int kLanesPerHead = kHalf / 4, kHeadsAtOnce = 32 / kLanesPerHead;       // queries: four (j, j + D/2) pairs a lane
   constexpr int kQPitch = 2 * D + 16;                                               // bytes
   static_assert(kMaxGroup * kQPitch <= kScratch && kMaxGroup * D * 2 <= kScratch && 4 * D <= kScratch, "scratch");
   extern __shared__ __align__(1024) uint8_t s_dyn[];
-  __shared__ int64_t s_warp[kStepWarps], s_before[kStepThreads];
-  __shared__ uint64_t s_bar[kStepWarps][4];                 // K of two units, V of two units
+  __shared__ int64_t s_warp[kWarps], s_before[kThreads];
+  __shared__ uint64_t s_bar[kWarps][4];                 // K of two units, V of two units
   __shared__ int s_abort;
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31, g = lane >> 2, t = lane & 3;
   const Line<kUnitRows> line{a, a.k_new != nullptr};
@@ -644,13 +648,13 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
   pdl_launch_dependents();
 
   // ---- the line, and this warp's piece of it
-  const int each = (a.n_prompts + kStepThreads - 1) / kStepThreads;
+  const int each = (a.n_prompts + kThreads - 1) / kThreads;
   int64_t mine = 0, total;
   for (int i = tid * each; i < min((tid + 1) * each, a.n_prompts); ++i) {
     const int len = checked_length(a.c, a.lengths, i, fresh, blockIdx.x == 0 ? a.status : nullptr);
     if (len >= 0) mine += line.line_units(len, a.own_start ? a.own_start[i] : 0);
   }
-  s_before[tid] = block_prefix<kStepThreads>(mine, s_warp, total);
+  s_before[tid] = block_prefix<kThreads>(mine, s_warp, total);
   __syncthreads();
   const int64_t per = (total + kPieces - 1) / kPieces;
   const int piece = warp * kSms + blockIdx.x;               // few units: a warp on each SM first
@@ -661,7 +665,7 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
   if (c.left <= 0) return;
   {
     int lo = 0;                         // last thread whose prompts begin at or before u0 (those without units come before it)
-    for (int w = 0; w < kStepWarps; ++w) lo += __popc(__ballot_sync(0xffffffffu, s_before[32 * w + lane] <= u0));
+    for (int w = 0; w < kWarps; ++w) lo += __popc(__ballot_sync(0xffffffffu, s_before[32 * w + lane] <= u0));
     --lo;
     int64_t at = u0 - s_before[lo];
     c.i = lo * each;
@@ -679,7 +683,7 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
   // ---- loads, which run ahead
   const uint32_t aligned = (smem_u32(s_dyn) + 1023u) & ~1023u;
   const uint32_t ring = aligned + warp * (4 * kHalfUnit);                           // K of two units, V of two units
-  uint8_t* scratch_p = s_dyn + (aligned - smem_u32(s_dyn)) + kStepWarps * (4 * kHalfUnit) + warp * kScratch;
+  uint8_t* scratch_p = s_dyn + (aligned - smem_u32(s_dyn)) + kWarps * (4 * kHalfUnit) + warp * kScratch;
   const uint32_t scratch = smem_u32(scratch_p), issue = elect_one(), lane_issue = lane < kSteps ? 1u : 0u;
   const int row_mask = (1 << a.c.page_shift) - 1;
   Place f = c;                          // where the copies are: unit f_at of the part f
@@ -735,26 +739,36 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
     const unsigned long long t0 = global_ns();
     while (global_ns() - t0 < 100000ull) {}
   };
-  while (true) {
-    // ---- a part of an item: queries
-    const bool begins = c.off == 0, ends = c.off + c.n == c.units, new_row = ends && fresh;
-    const __nv_bfloat16* q_row = a.q_new + (int64_t)c.i * a.q_stride + (int64_t)c.kvh * a.group * D;
-    uint2 lo2[kMaxGroup / kHeadsAtOnce], hi2[kMaxGroup / kHeadsAtOnce], new_lo, new_hi, new_v;
+  // What a part of an item needs beside its rows: four (j, j + D/2) pairs of the lane's heads, and of the new token.
+  struct Raw { uint2 lo[kMaxGroup / kHeadsAtOnce], hi[kMaxGroup / kHeadsAtOnce], new_lo, new_hi, new_v; };
+  auto ends_item = [&](const Place& p) { return p.off + p.n == p.units; };
+  auto fetch = [&](Raw& r, const Place& p) {
+    const __nv_bfloat16* q_row = a.q_new + (int64_t)p.i * a.q_stride + (int64_t)p.kvh * a.group * D;
 #pragma unroll
     for (int x = 0; x < kMaxGroup / kHeadsAtOnce; ++x) {
       const int h = x * kHeadsAtOnce + lane / kLanesPerHead;
-      lo2[x] = hi2[x] = make_uint2(0u, 0u);
+      r.lo[x] = r.hi[x] = make_uint2(0u, 0u);
       if (h < a.group) {
-        lo2[x] = *reinterpret_cast<const uint2*>(q_row + h * D + j0);
-        hi2[x] = *reinterpret_cast<const uint2*>(q_row + h * D + j0 + kHalf);
+        r.lo[x] = *reinterpret_cast<const uint2*>(q_row + h * D + j0);
+        r.hi[x] = *reinterpret_cast<const uint2*>(q_row + h * D + j0 + kHalf);
       }
     }
-    if (new_row) {
-      const __nv_bfloat16* k_row = a.k_new + (int64_t)c.i * a.k_stride + c.kvh * D;
-      new_lo = *reinterpret_cast<const uint2*>(k_row + j0);
-      new_hi = *reinterpret_cast<const uint2*>(k_row + j0 + kHalf);
-      new_v = *reinterpret_cast<const uint2*>(a.v_new + (int64_t)c.i * a.v_stride + c.kvh * D + 4 * (lane % (D / 4)));
+    if (fresh && ends_item(p)) {
+      const __nv_bfloat16* k_row = a.k_new + (int64_t)p.i * a.k_stride + p.kvh * D;
+      r.new_lo = *reinterpret_cast<const uint2*>(k_row + j0);
+      r.new_hi = *reinterpret_cast<const uint2*>(k_row + j0 + kHalf);
+      r.new_v = *reinterpret_cast<const uint2*>(a.v_new + (int64_t)p.i * a.v_stride + p.kvh * D + 4 * (lane % (D / 4)));
     }
+  };
+  Raw raw, raw_next;
+  fetch(raw_next, c);
+  while (true) {
+    // ---- a part of an item; the queries of the next one are on their way meanwhile
+    const bool begins = c.off == 0, ends = ends_item(c), new_row = ends && fresh;
+    raw = raw_next;
+    Place next = c;
+    line.advance(next);
+    if (next.n > 0) fetch(raw_next, next);
     // (m, l) and o over the rows that the prompt shares, where this part is the item's first
     float m[2] = {kNoScore, kNoScore}, l[2] = {0.f, 0.f}, acc[D / 16][4];
 #pragma unroll
@@ -790,13 +804,13 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
     const float k_scale = kE4m3 ? a.c.k_scale[c.kvh] : 1.f, v_scale = kE4m3 ? a.c.v_scale[c.kvh] : 1.f;
     uint32_t qh[D / 8], ql[D / 8];
     float scale[2] = {a.scale_log2, a.scale_log2};
-    // the upper parts through the scratch memory, then the lower ones, which wait in lo2 and hi2
+    // the upper parts through the scratch memory, then the lower ones, which wait in `raw`
 #pragma unroll
     for (int x = 0; x < kMaxGroup / kHeadsAtOnce; ++x) {
       if (x * kHeadsAtOnce >= a.group) break;
       const int h = x * kHeadsAtOnce + lane / kLanesPerHead;
       float p[4], y[4];
-      turn(lo2[x], hi2[x], p, y);
+      turn(raw.lo[x], raw.hi[x], p, y);
       if constexpr (kE4m3) {
         // f16 has 5 exponent bits: a query is brought to below 2 by a power of two (of up to 2^120: the rest f16 has room
         // for), which goes into its factor
@@ -818,8 +832,8 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
       const uint32_t w[4] = {R::high(p[0], p[1]), R::high(p[2], p[3]), R::high(y[0], y[1]), R::high(y[2], y[3])};
       *reinterpret_cast<uint2*>(scratch_p + h * kQPitch + 2 * j0) = make_uint2(w[0], w[1]);
       *reinterpret_cast<uint2*>(scratch_p + h * kQPitch + 2 * (j0 + kHalf)) = make_uint2(w[2], w[3]);
-      lo2[x] = make_uint2(R::low(p[0], p[1], w[0]), R::low(p[2], p[3], w[1]));
-      hi2[x] = make_uint2(R::low(y[0], y[1], w[2]), R::low(y[2], y[3], w[3]));
+      raw.lo[x] = make_uint2(R::low(p[0], p[1], w[0]), R::low(p[2], p[3], w[1]));
+      raw.hi[x] = make_uint2(R::low(y[0], y[1], w[2]), R::low(y[2], y[3], w[3]));
     }
     __syncwarp();
     R::load_q(qh, scratch + g * kQPitch, t);
@@ -829,8 +843,8 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
       for (int x = 0; x < kMaxGroup / kHeadsAtOnce; ++x) {
         if (x * kHeadsAtOnce >= a.group) break;
         const int h = x * kHeadsAtOnce + lane / kLanesPerHead;
-        *reinterpret_cast<uint2*>(scratch_p + h * kQPitch + 2 * j0) = lo2[x];
-        *reinterpret_cast<uint2*>(scratch_p + h * kQPitch + 2 * (j0 + kHalf)) = hi2[x];
+        *reinterpret_cast<uint2*>(scratch_p + h * kQPitch + 2 * j0) = raw.lo[x];
+        *reinterpret_cast<uint2*>(scratch_p + h * kQPitch + 2 * (j0 + kHalf)) = raw.hi[x];
       }
       __syncwarp();
       R::load_q(ql, scratch + g * kQPitch, t);
@@ -907,8 +921,8 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
     }
     if (new_row) {                      // the new token, and its rows of the pages
       float p[4], y[4];
-      turn(new_lo, new_hi, p, y);
-      const float2 v0 = unpack_bf16(new_v.x), v1 = unpack_bf16(new_v.y);
+      turn(raw.new_lo, raw.new_hi, p, y);
+      const float2 v0 = unpack_bf16(raw.new_v.x), v1 = unpack_bf16(raw.new_v.y);
       if constexpr (kE4m3) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) { p[e] = __fdiv_rn(p[e], k_scale); y[e] = __fdiv_rn(y[e], k_scale); }
@@ -924,7 +938,7 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
           *reinterpret_cast<uint2*>(scratch_p + 2 * j0) = make_uint2(round_bf16(p[0], p[1]), round_bf16(p[2], p[3]));
           *reinterpret_cast<uint2*>(scratch_p + 2 * (j0 + kHalf)) = make_uint2(round_bf16(y[0], y[1]), round_bf16(y[2], y[3]));
         }
-        if (lane < D / 4) *reinterpret_cast<uint2*>(scratch_p + 2 * D + 8 * lane) = new_v;
+        if (lane < D / 4) *reinterpret_cast<uint2*>(scratch_p + 2 * D + 8 * lane) = raw.new_v;
       }
       __syncwarp();
       float s[1][4];
@@ -974,13 +988,13 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
       if (begins && lane == 0)          // the pieces over which the item goes on: units behind this one's end
         a.cut[piece] = make_int4(c.i, c.kvh, 1 + (int)((c.units - c.n + per - 1) / per), 0);
     }
-    line.advance(c);
-    if (c.n == 0) return;
+    if (next.n == 0) return;
+    c = next;
   }
 }
 
-// Joins the parts of the items that are cut: a CTA for a query head of the KV head, which takes every kCombineBlocks-th piece in which
-// such an item may begin. Its warps share the parts: one prompt alone may have hundreds.
+// Joins the parts of the items that are cut: a CTA for a query head of the KV head and a piece in which such an item may begin (the
+// others leave at once). Its warps share the parts: one prompt alone may have hundreds.
 template <int D>
 __global__ void __launch_bounds__(kCombineThreads)
 paged_combine_kernel(const __grid_constant__ PagedArgs a) {
@@ -989,72 +1003,70 @@ paged_combine_kernel(const __grid_constant__ PagedArgs a) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, h = blockIdx.y;
   pdl_wait();                           // the parts come from the kernels before this one
   pdl_launch_dependents();
-  for (int piece = blockIdx.x; piece < kPieces; piece += kCombineBlocks) {
-    const int4 cut = a.cut[piece];
-    if (cut.z == 0) continue;
-    float mm = kNoScore, ll = 0.f, oo[E];
+  const int piece = blockIdx.x;
+  const int4 cut = a.cut[piece];
+  if (cut.z == 0) return;
+  float mm = kNoScore, ll = 0.f, oo[E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) oo[e] = 0.f;
-    const int n_all = cut.z;
-    const int64_t first = 2 * (int64_t)piece;
-    auto slot = [&](int part) { return (first + (part == 0 ? 1 : 2 * part)) * a.group + h; };
-    constexpr int kAtOnce = 4;          // parts whose loads are under way together
-    for (int base = warp; base < n_all; base += kAtOnce * kWarps) {
-      float2 ml[kAtOnce];
-      float p[kAtOnce][E];
+  for (int e = 0; e < E; ++e) oo[e] = 0.f;
+  const int n_all = cut.z;
+  const int64_t first = 2 * (int64_t)piece;
+  auto slot = [&](int part) { return (first + (part == 0 ? 1 : 2 * part)) * a.group + h; };
+  constexpr int kAtOnce = 4;          // parts whose loads are under way together
+  for (int base = warp; base < n_all; base += kAtOnce * kWarps) {
+    float2 ml[kAtOnce];
+    float p[kAtOnce][E];
 #pragma unroll
-      for (int c = 0; c < kAtOnce; ++c) {
-        ml[c] = make_float2(kNoScore, 0.f);
+    for (int c = 0; c < kAtOnce; ++c) {
+      ml[c] = make_float2(kNoScore, 0.f);
 #pragma unroll
-        for (int e = 0; e < E; ++e) p[c][e] = 0.f;
-        if (base + c * kWarps >= n_all) continue;
-        const int64_t at = slot(base + c * kWarps);
-        ml[c] = a.part_ml[at];
-        const float* src = a.part_o + at * D + E * lane;
-        if constexpr (E == 4) {
-          const float4 x = *reinterpret_cast<const float4*>(src);
-          p[c][0] = x.x; p[c][1] = x.y; p[c][2] = x.z; p[c][3] = x.w;
-        } else {
-          const float2 x = *reinterpret_cast<const float2*>(src);
-          p[c][0] = x.x; p[c][1] = x.y;
-        }
-      }
-      float m_new = mm;
-#pragma unroll
-      for (int c = 0; c < kAtOnce; ++c) m_new = fmaxf(m_new, ml[c].x);
-      const float alpha = ex2(mm - m_new);
-      mm = m_new;
-      ll *= alpha;
-#pragma unroll
-      for (int e = 0; e < E; ++e) oo[e] *= alpha;
-#pragma unroll
-      for (int c = 0; c < kAtOnce; ++c) {
-        const float f = ex2(ml[c].x - m_new);
-        ll += ml[c].y * f;
-#pragma unroll
-        for (int e = 0; e < E; ++e) oo[e] += p[c][e] * f;
+      for (int e = 0; e < E; ++e) p[c][e] = 0.f;
+      if (base + c * kWarps >= n_all) continue;
+      const int64_t at = slot(base + c * kWarps);
+      ml[c] = a.part_ml[at];
+      const float* src = a.part_o + at * D + E * lane;
+      if constexpr (E == 4) {
+        const float4 x = *reinterpret_cast<const float4*>(src);
+        p[c][0] = x.x; p[c][1] = x.y; p[c][2] = x.z; p[c][3] = x.w;
+      } else {
+        const float2 x = *reinterpret_cast<const float2*>(src);
+        p[c][0] = x.x; p[c][1] = x.y;
       }
     }
-    if (lane == 0) { s_m[warp] = mm; s_l[warp] = ll; }
+    float m_new = mm;
 #pragma unroll
-    for (int e = 0; e < E; ++e) s_o[warp][E * lane + e] = oo[e];
-    __syncthreads();
-    if (threadIdx.x < D) {
-      mm = s_m[0];
+    for (int c = 0; c < kAtOnce; ++c) m_new = fmaxf(m_new, ml[c].x);
+    const float alpha = ex2(mm - m_new);
+    mm = m_new;
+    ll *= alpha;
 #pragma unroll
-      for (int w = 1; w < kWarps; ++w) mm = fmaxf(mm, s_m[w]);
-      ll = 0.f;
-      float o = 0.f;
+    for (int e = 0; e < E; ++e) oo[e] *= alpha;
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) {
-        const float f = ex2(s_m[w] - mm);
-        ll += s_l[w] * f;
-        o += s_o[w][threadIdx.x] * f;
-      }
-      // (an item that is cut has rows)
-      a.o[((int64_t)cut.x * a.n_q_heads + cut.y * a.group + h) * D + threadIdx.x] = __float2bfloat16_rn(o / ll);
+    for (int c = 0; c < kAtOnce; ++c) {
+      const float f = ex2(ml[c].x - m_new);
+      ll += ml[c].y * f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) oo[e] += p[c][e] * f;
     }
-    __syncthreads();
+  }
+  if (lane == 0) { s_m[warp] = mm; s_l[warp] = ll; }
+#pragma unroll
+  for (int e = 0; e < E; ++e) s_o[warp][E * lane + e] = oo[e];
+  __syncthreads();
+  if (threadIdx.x < D) {
+    mm = s_m[0];
+#pragma unroll
+    for (int w = 1; w < kWarps; ++w) mm = fmaxf(mm, s_m[w]);
+    ll = 0.f;
+    float o = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+      const float f = ex2(s_m[w] - mm);
+      ll += s_l[w] * f;
+      o += s_o[w][threadIdx.x] * f;
+    }
+    // (an item that is cut has rows)
+    a.o[((int64_t)cut.x * a.n_q_heads + cut.y * a.group + h) * D + threadIdx.x] = __float2bfloat16_rn(o / ll);
   }
 }
 
@@ -1293,20 +1305,21 @@ bool page_map(CUtensorMap* map, const void* pages, const PagedArgs& a, int d, bo
 
 template <int D, bool kE4m3>
 cudaError_t launch_paged_decode(const PagedArgs& a, const SharedPlan& plan, cudaStream_t s) {
+  constexpr int kWarps = Rows<D, kE4m3>::kWarps, kSmem = 1024 + kWarps * (4 * kHalfUnit + kScratch);     // rings on 1024-byte boundaries
   static DeviceOnce configured;
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   if (!configured.done(dev)) {
-    e = cudaFuncSetAttribute(paged_decode_kernel<D, kE4m3>, cudaFuncAttributeMaxDynamicSharedMemorySize, kStepSmem);
+    e = cudaFuncSetAttribute(paged_decode_kernel<D, kE4m3>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
     if (e != cudaSuccess) return e;
     configured.mark(dev);
   }
   CUtensorMap mk, mv;
   if (!page_map(&mk, a.c.k_pages, a, D, kE4m3) || !page_map(&mv, a.c.v_pages, a, D, kE4m3)) return cudaErrorInvalidValue;
-  e = launch_dependent(paged_decode_kernel<D, kE4m3>, dim3(kSms), dim3(kStepThreads), (size_t)kStepSmem, s, mk, mv, a, plan);
+  e = launch_dependent(paged_decode_kernel<D, kE4m3>, dim3(kSms), dim3(32 * kWarps), (size_t)kSmem, s, mk, mv, a, plan);
   if (e != cudaSuccess) return e;
-  return launch_dependent(paged_combine_kernel<D>, dim3(kCombineBlocks, a.group), dim3(kCombineThreads), 0, s, a);
+  return launch_dependent(paged_combine_kernel<D>, dim3(kSms * kWarps, a.group), dim3(kCombineThreads), 0, s, a);
 }
 
 template <int D>
@@ -1414,8 +1427,8 @@ PagedWorkspace paged_workspace(const pp_attn_params& p, int32_t k, int32_t n_gro
     at = (at + bytes + 255) & ~size_t(255);
     return here;
   };
-  const size_t parts = 2 * (size_t)kPieces * (p.n_q_heads / p.n_kv_heads);
-  L.cut = take((size_t)kPieces * sizeof(int4));
+  const size_t parts = 2 * (size_t)kMostPieces * (p.n_q_heads / p.n_kv_heads);
+  L.cut = take((size_t)kMostPieces * sizeof(int4));
   L.part_ml = take(parts * sizeof(float2));
   L.part_o = take(parts * p.head_dim * sizeof(float));
   if (n_groups > 0) {
