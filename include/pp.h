@@ -337,8 +337,8 @@ enum {
  *   k_new, v_new device bf16, row r at r * k_stride / r * v_stride elements, [Hkv, D] within a row; a stride of 0 stands for
  *                Hkv * D, others are multiples of 8 and at least that, so that both may be slices of one projection
  *   device_status device int32 or NULL, see PP_PAGED_*; the caller zeroes and reads it
- * Arithmetic: rotation in fp32 with one rounding, to bf16 or, after a division by the scale, to e4m3 (to nearest, what is beyond
- * its range to +-448, a NaN stays one); the bf16 keys are bit for bit those of the prefill. Two rows of the same prompt and
+ * Arithmetic: rotation in fp32 with one rounding, to bf16 or, times the reciprocal of the scale, to e4m3 (to nearest, what is
+ * beyond its range to +-448, a NaN stays one); the bf16 keys are bit for bit those of the prefill. Two rows of the same prompt and
  * position in one call leave any mixture of the two. A row may be appended again. Asynchronous on `stream`.
  * Errors: PP_ERR_INVALID_ARG, PP_ERR_UNSUPPORTED (head_dim, page_size, type, device), PP_ERR_ALIGNMENT, PP_ERR_CUDA.
  */

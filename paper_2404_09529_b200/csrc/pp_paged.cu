@@ -60,10 +60,14 @@ __device__ __forceinline__ uint32_t round_e4m3(float a, float b, float c, float 
 // ------------------------------------------------------------------------------------------
 // Rows into pages
 // ------------------------------------------------------------------------------------------
-// A copy with a rotation in it, bound by HBM: a CTA takes as many rows as make 4096 elements of K (one 8 + 8 element pair of
-// pieces per thread, two pieces of V), finds where they go, and has all of its loads under way before it needs the angles,
-// which are computed once for all heads of a row.
-constexpr int kAppendThreads = 256;
+// A copy with a rotation in it, bound by HBM: a CTA takes as many rows (or heads of one) as make 2048 elements of K. A thread has one pair of 8-element
+// pieces of K (c and D/2 + c) and two pieces of V of the same row, so that all it needs is that row's prompt and position:
+// its loads, the page's number and the angles (once for all heads of a row, through shared memory) are then under way together.
+// 17 554 rows of 32 heads of 128 take 89 us (6.5 TB/s; 114 with the row's place found first and handed round), 44 k short rows of
+// 8 heads of 64 into 8 bits 33 us (4.1 TB/s, was 55), where instructions count: 430 a thread, a quarter of them for the angle, and as
+// many for the conversions.
+constexpr int kAppendThreads = 128;
+constexpr int kAppendElements = 16 * kAppendThreads;        // of K in a CTA: several rows, or some heads of one
 constexpr int kAppendMaxRows = 16;
 
 struct AppendArgs {
@@ -71,132 +75,120 @@ struct AppendArgs {
   const int32_t *prompt, *position;
   const __nv_bfloat16 *k_new, *v_new;
   int64_t k_stride, v_stride, n_rows;
-  int32_t n_prompts, n_kv_heads, rows_per_cta;
+  int32_t n_prompts, n_kv_heads, rows_per_cta, heads_per_cta;
   bool rotate;
   int32_t* status;
   RopeAngles angles;
 };
 
+__device__ __forceinline__ void widen8(const uint4& x, float (&f)[8]) {
+  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float2 y = unpack_bf16(w[e]);
+    f[2 * e] = y.x;
+    f[2 * e + 1] = y.y;
+  }
+}
+__device__ __forceinline__ uint4 narrow8(const float (&f)[8]) {
+  return make_uint4(round_bf16(f[0], f[1]), round_bf16(f[2], f[3]), round_bf16(f[4], f[5]), round_bf16(f[6], f[7]));
+}
+__device__ __forceinline__ uint2 narrow8(const float (&f)[8], float per_scale) {
+  return make_uint2(round_e4m3(f[0] * per_scale, f[1] * per_scale, f[2] * per_scale, f[3] * per_scale),
+                    round_e4m3(f[4] * per_scale, f[5] * per_scale, f[6] * per_scale, f[7] * per_scale));
+}
+
 template <int D, bool kE4m3>
-__global__ void __launch_bounds__(kAppendThreads)
+__global__ void __launch_bounds__(kAppendThreads, kE4m3 ? 8 : 10)
 append_kernel(const __grid_constant__ AppendArgs a) {
-  constexpr int kHalf = D / 2, kSize = kE4m3 ? 1 : 2;
-  constexpr int kKUnits = kHalf / 8, kVUnits = D / 8;       // per head: pieces of 8 + 8 elements, pieces of 8 elements
-  __shared__ int32_t s_pos[kAppendMaxRows];
-  __shared__ int64_t s_to[kAppendMaxRows];                  // byte offset of the row (head 0) in either pool, -1: not written
-  __shared__ float s_cos[kAppendMaxRows][kHalf], s_sin[kAppendMaxRows][kHalf];
+  constexpr int kHalf = D / 2, kSize = kE4m3 ? 1 : 2, kUnits = kHalf / 8;      // pairs of pieces per head
+  __shared__ __align__(16) float s_cos[kAppendMaxRows][kHalf], s_sin[kAppendMaxRows][kHalf];
   const int tid = threadIdx.x;
   const int64_t row0 = (int64_t)blockIdx.x * a.rows_per_cta;
-  const int rows = (int)min((int64_t)a.rows_per_cta, a.n_rows - row0);
+  const int rows = (int)min((int64_t)a.rows_per_cta, a.n_rows - row0), head0 = blockIdx.y * a.heads_per_cta;
+  const int units = min(a.heads_per_cta, a.n_kv_heads - head0) * kUnits;
   pdl_launch_dependents();
   pdl_wait();
-  if (tid < rows) {
-    const int prompt = a.prompt[row0 + tid];
-    int64_t to = -1;
-    int pos = 0;
+  for (int u0 = 0; u0 < rows * units; u0 += kAppendThreads) {
+    const int u = u0 + tid, r = u / units, w = u - r * units + head0 * kUnits, head = w / kUnits, c = 8 * (w - head * kUnits);
+    int prompt = -1, pos = 0;
+    if (r < rows) {
+      prompt = a.prompt[row0 + r];
+      pos = a.position[row0 + r];
+    }
+    if (prompt >= a.n_prompts) {
+      if (w == 0) note_status(a.status, PP_PAGED_BAD_PROMPT);
+      prompt = -1;
+    }
+    if (prompt >= 0 && (pos < 0 || (pos >> a.c.page_shift) >= a.c.table_stride)) {
+      if (w == 0) note_status(a.status, PP_PAGED_BAD_POSITION);
+      prompt = -1;
+    }
+    int page = 0;
+    uint4 lo, hi, v[2];
     if (prompt >= 0) {
-      pos = a.position[row0 + tid];
-      if (prompt >= a.n_prompts) note_status(a.status, PP_PAGED_BAD_PROMPT);
-      else if (pos < 0 || (pos >> a.c.page_shift) >= a.c.table_stride) note_status(a.status, PP_PAGED_BAD_POSITION);
-      else {
-        const int page = a.c.table[(int64_t)prompt * a.c.table_stride + (pos >> a.c.page_shift)];
-        if ((unsigned)page >= (unsigned)a.c.n_pages) note_status(a.status, PP_PAGED_BAD_PAGE);
-        else to = (int64_t)page * a.c.page_stride + (int64_t)(pos & ((1 << a.c.page_shift) - 1)) * a.c.row_stride;
-      }
+      page = a.c.table[(int64_t)prompt * a.c.table_stride + (pos >> a.c.page_shift)];
+      const __nv_bfloat16 *k = a.k_new + (row0 + r) * a.k_stride + head * D + c, *vs = a.v_new + (row0 + r) * a.v_stride + 16 * w;
+      lo = load16(k);
+      hi = load16(k + kHalf);
+      v[0] = load16(vs);
+      v[1] = load16(vs + 8);
     }
-    s_pos[tid] = pos;
-    s_to[tid] = to;
-  }
-  __syncthreads();
-  const int k_units = a.n_kv_heads * kKUnits, v_units = a.n_kv_heads * kVUnits;
-  const int trips = (rows * k_units + kAppendThreads - 1) / kAppendThreads;
-  for (int trip = 0; trip < trips; ++trip) {
-    const int u = trip * kAppendThreads + tid;
-    // K: elements 8c .. and D/2 + 8c ..; V: the same number of pieces, two per thread
-    const int r = u / k_units, w = u - r * k_units, head = w / kKUnits, c = w - head * kKUnits;
-    const bool k_here = r < rows && s_to[r] >= 0;
-    uint4 lo = make_uint4(0u, 0u, 0u, 0u), hi = lo, v[2] = {lo, lo};
-    int vr[2], vw[2];
-    bool v_here[2];
-    if (k_here) {
-      const __nv_bfloat16* p = a.k_new + (row0 + r) * a.k_stride + head * D + 8 * c;
-      lo = load16(p);
-      hi = load16(p + kHalf);
-    }
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const int n = trip * 2 * kAppendThreads + 2 * tid + x;      // (a thread's two pieces stand next to one another)
-      vr[x] = n / v_units;
-      vw[x] = n - vr[x] * v_units;
-      v_here[x] = vr[x] < rows && s_to[vr[x]] >= 0;
-      if (v_here[x]) v[x] = load16(a.v_new + (row0 + vr[x]) * a.v_stride + 8 * vw[x]);
-    }
-    if (trip == 0) {
+    if (u0 == 0) {
       if (a.rotate) {
         for (int n = tid; n < rows * kHalf; n += kAppendThreads) {
           const int ar = n / kHalf, j = n - ar * kHalf;
-          float cs, sn;
-          angle(s_pos[ar], a.angles.inv_freq[j], cs, sn);
-          s_cos[ar][j] = cs;
-          s_sin[ar][j] = sn;
+          angle(a.position[row0 + ar], a.angles.inv_freq[j], s_cos[ar][j], s_sin[ar][j]);
         }
       }
       __syncthreads();
     }
-    if (k_here) {
-      char* to = a.c.k_pages + s_to[r] + (int64_t)head * a.c.head_stride + 8 * c * kSize;
-      if (a.rotate || kE4m3) {
-        float x[8], y[8];
-        const uint32_t lw[4] = {lo.x, lo.y, lo.z, lo.w}, hw[4] = {hi.x, hi.y, hi.z, hi.w};
+    if (prompt < 0) continue;
+    if ((unsigned)page >= (unsigned)a.c.n_pages) {
+      if (w == 0) note_status(a.status, PP_PAGED_BAD_PAGE);
+      continue;
+    }
+    const int64_t to = (int64_t)page * a.c.page_stride + (int64_t)(pos & ((1 << a.c.page_shift) - 1)) * a.c.row_stride;
+    const int v_head = 16 * w / D, v_at = 16 * w - v_head * D;
+    char *k_to = a.c.k_pages + to + (int64_t)head * a.c.head_stride + c * kSize, *v_to = a.c.v_pages + to + (int64_t)v_head * a.c.head_stride + v_at * kSize;
+    if (a.rotate || kE4m3) {
+      float x[8], y[8];
+      widen8(lo, x);
+      widen8(hi, y);
+      if (a.rotate) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float2 l2 = unpack_bf16(lw[e]), h2 = unpack_bf16(hw[e]);
-          x[2 * e] = l2.x; x[2 * e + 1] = l2.y;
-          y[2 * e] = h2.x; y[2 * e + 1] = h2.y;
-        }
-        if (a.rotate) {
+        for (int e = 0; e < 8; e += 4) {
+          const float4 c4 = *reinterpret_cast<const float4*>(&s_cos[r][c + e]), s4 = *reinterpret_cast<const float4*>(&s_sin[r][c + e]);
+          const float cs[4] = {c4.x, c4.y, c4.z, c4.w}, sn[4] = {s4.x, s4.y, s4.z, s4.w};
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float cs = s_cos[r][8 * c + e], sn = s_sin[r][8 * c + e], p = x[e], q = y[e];
-            x[e] = turn_lo(p, q, cs, sn);
-            y[e] = turn_hi(p, q, cs, sn);
+          for (int n = 0; n < 4; ++n) {
+            const float p = x[e + n], q = y[e + n];
+            x[e + n] = turn_lo(p, q, cs[n], sn[n]);
+            y[e + n] = turn_hi(p, q, cs[n], sn[n]);
           }
         }
-        if constexpr (kE4m3) {
-          const float scale = a.c.k_scale[head];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) { x[e] = __fdiv_rn(x[e], scale); y[e] = __fdiv_rn(y[e], scale); }
-          *reinterpret_cast<uint2*>(to) = make_uint2(round_e4m3(x[0], x[1], x[2], x[3]), round_e4m3(x[4], x[5], x[6], x[7]));
-          *reinterpret_cast<uint2*>(to + kHalf) = make_uint2(round_e4m3(y[0], y[1], y[2], y[3]), round_e4m3(y[4], y[5], y[6], y[7]));
-        } else {
-          lo = make_uint4(round_bf16(x[0], x[1]), round_bf16(x[2], x[3]), round_bf16(x[4], x[5]), round_bf16(x[6], x[7]));
-          hi = make_uint4(round_bf16(y[0], y[1]), round_bf16(y[2], y[3]), round_bf16(y[4], y[5]), round_bf16(y[6], y[7]));
-        }
       }
-      if constexpr (!kE4m3) {
-        *reinterpret_cast<uint4*>(to) = lo;
-        *reinterpret_cast<uint4*>(to + kHalf * kSize) = hi;
+      if constexpr (kE4m3) {
+        const float per_scale = __frcp_rn(a.c.k_scale[head]);
+        *reinterpret_cast<uint2*>(k_to) = narrow8(x, per_scale);
+        *reinterpret_cast<uint2*>(k_to + kHalf) = narrow8(y, per_scale);
+      } else {
+        lo = narrow8(x);
+        hi = narrow8(y);
       }
     }
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      if (!v_here[x]) continue;
-      const int vh = vw[x] / kVUnits, vc = vw[x] - vh * kVUnits;
-      char* to = a.c.v_pages + s_to[vr[x]] + (int64_t)vh * a.c.head_stride + 8 * vc * kSize;
-      if constexpr (kE4m3) {
-        const float scale = a.c.v_scale[vh];
-        const uint32_t w4[4] = {v[x].x, v[x].y, v[x].z, v[x].w};
-        float e[8];
-#pragma unroll
-        for (int n = 0; n < 4; ++n) {
-          const float2 f = unpack_bf16(w4[n]);
-          e[2 * n] = __fdiv_rn(f.x, scale);
-          e[2 * n + 1] = __fdiv_rn(f.y, scale);
-        }
-        *reinterpret_cast<uint2*>(to) = make_uint2(round_e4m3(e[0], e[1], e[2], e[3]), round_e4m3(e[4], e[5], e[6], e[7]));
-      } else {
-        *reinterpret_cast<uint4*>(to) = v[x];
-      }
+    if constexpr (kE4m3) {
+      const float per_scale = __frcp_rn(a.c.v_scale[v_head]);
+      float x[8], y[8];
+      widen8(v[0], x);
+      widen8(v[1], y);
+      const uint2 p = narrow8(x, per_scale), q = narrow8(y, per_scale);
+      *reinterpret_cast<uint4*>(v_to) = make_uint4(p.x, p.y, q.x, q.y);
+    } else {
+      *reinterpret_cast<uint4*>(k_to) = lo;
+      *reinterpret_cast<uint4*>(k_to + kHalf * kSize) = hi;
+      *reinterpret_cast<uint4*>(v_to) = v[0];
+      *reinterpret_cast<uint4*>(v_to + 16) = v[1];
     }
   }
 }
@@ -924,15 +916,16 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
       turn(raw.new_lo, raw.new_hi, p, y);
       const float2 v0 = unpack_bf16(raw.new_v.x), v1 = unpack_bf16(raw.new_v.y);
       if constexpr (kE4m3) {
+        const float per_k = __frcp_rn(k_scale), per_v = __frcp_rn(v_scale);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) { p[e] = __fdiv_rn(p[e], k_scale); y[e] = __fdiv_rn(y[e], k_scale); }
+        for (int e = 0; e < 4; ++e) { p[e] *= per_k; y[e] *= per_k; }
         if (lane < kLanesPerHead) {
           *reinterpret_cast<uint32_t*>(scratch_p + j0) = round_e4m3(p[0], p[1], p[2], p[3]);
           *reinterpret_cast<uint32_t*>(scratch_p + j0 + kHalf) = round_e4m3(y[0], y[1], y[2], y[3]);
         }
         if (lane < D / 4)
           *reinterpret_cast<uint32_t*>(scratch_p + D + 4 * lane) =
-              round_e4m3(__fdiv_rn(v0.x, v_scale), __fdiv_rn(v0.y, v_scale), __fdiv_rn(v1.x, v_scale), __fdiv_rn(v1.y, v_scale));
+              round_e4m3(v0.x * per_v, v0.y * per_v, v1.x * per_v, v1.y * per_v);
       } else {
         if (lane < kLanesPerHead) {
           *reinterpret_cast<uint2*>(scratch_p + 2 * j0) = make_uint2(round_bf16(p[0], p[1]), round_bf16(p[2], p[3]));
@@ -1468,7 +1461,12 @@ extern "C" int pp_paged_append(const pp_attn_params* params, const pp_paged_cach
   if (!pp::aligned(k_new, 16) || !pp::aligned(v_new, 16) || !pp::aligned(prompt, 4) || !pp::aligned(position, 4) || !pp::aligned(device_status, 4))
     return PP_ERR_ALIGNMENT;
   if (n_rows == 0) return PP_OK;
-  a.rows_per_cta = (int32_t)std::min<int64_t>(std::max<int64_t>(4096 / dense, 1), pp::kAppendMaxRows);
+  a.rows_per_cta = (int32_t)std::min<int64_t>(std::max<int64_t>(pp::kAppendElements / dense, 1), pp::kAppendMaxRows);
+  // The heads of one long row are shared out to several CTAs only while the GPU has room for all of them at once: each needs the row's
+  // angles. (64 rows of 32 heads of 128: 3.2 -> 2.5 us; 17 554 of them 89 -> 94.)
+  a.heads_per_cta = std::min(params->n_kv_heads, pp::kAppendElements / params->head_dim);
+  if (n_rows * ((params->n_kv_heads + a.heads_per_cta - 1) / a.heads_per_cta) > 8 * pp::kSms) a.heads_per_cta = params->n_kv_heads;
+  const int32_t head_blocks = (params->n_kv_heads + a.heads_per_cta - 1) / a.heads_per_cta;
   const int64_t grid = (n_rows + a.rows_per_cta - 1) / a.rows_per_cta;
   if (grid > INT32_MAX) return PP_ERR_UNSUPPORTED;
   if ((st = pp::check_paged_device()) != PP_OK) return st;
@@ -1485,7 +1483,7 @@ extern "C" int pp_paged_append(const pp_attn_params* params, const pp_paged_cach
   a.angles = pp::rope_angles(params->rope_base, params->head_dim);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const bool e4m3 = cache->type == PP_CACHE_E4M3;
-  auto launch = [&](auto kernel) { return pp::launch_dependent(kernel, dim3((unsigned)grid), dim3(pp::kAppendThreads), 0, s, a); };
+  auto launch = [&](auto kernel) { return pp::launch_dependent(kernel, dim3((unsigned)grid, (unsigned)head_blocks), dim3(pp::kAppendThreads), 0, s, a); };
   const cudaError_t e = params->head_dim == 128 ? (e4m3 ? launch(pp::append_kernel<128, true>) : launch(pp::append_kernel<128, false>))
                                                 : (e4m3 ? launch(pp::append_kernel<64, true>) : launch(pp::append_kernel<64, false>));
   return e == cudaSuccess ? PP_OK : pp::note_cuda_error((int)e, "append kernel launch");
