@@ -1148,22 +1148,25 @@ shared_plan_kernel(const __grid_constant__ PlanArgs p) {
   __syncthreads();
   const int page_mask = (1 << a.c.page_shift) - 1;
   const int each = (n + kPlanThreads - 1) / kPlanThreads, g0 = min(tid * each, n), g1 = min(g0 + each, n);
-  int64_t units = 0;
+  int64_t units = 0, parts = 0;
   for (int g = g0; g < g1; ++g) {
     const int prompts = bad ? 0 : s_ptr[g + 1] - s_ptr[g];
     const int rows = prompts > 0 && s_lead[g] < k ? s_rows[g] & ~page_mask : 0;      // (a group may be all rows of no prompt)
     s_rows[g] = rows;
     const int tiles = (rows + kSharedTileKeys - 1) / kSharedTileKeys;
     units += (int64_t)tiles * ((prompts * a.group + kSharedTileRows - 1) / kSharedTileRows) * a.n_kv_heads;
+    parts += (int64_t)shared_part_rows(prompts * a.group) * a.n_kv_heads;
   }
-  int64_t all, at = block_prefix<kPlanThreads>(units, s_warp, all);
+  int64_t all, none, at = block_prefix<kPlanThreads>(units, s_warp, all), part = block_prefix<kPlanThreads>(parts, s_warp, none);
   for (int g = g0; g < g1; ++g) {
     const int prompts = bad ? 0 : s_ptr[g + 1] - s_ptr[g], tiles = (s_rows[g] + kSharedTileKeys - 1) / kSharedTileKeys;
     plan.unit_start[g] = at;
+    plan.part_start[g] = part;
     plan.key_tiles[g] = tiles;
     plan.shared_rows[g] = s_rows[g];
     plan.lead[g] = s_lead[g];
     at += (int64_t)tiles * ((prompts * a.group + kSharedTileRows - 1) / kSharedTileRows) * a.n_kv_heads;
+    part += (int64_t)shared_part_rows(prompts * a.group) * a.n_kv_heads;
   }
   if (tid == 0) {
     plan.unit_start[n] = all;
@@ -1194,31 +1197,50 @@ shared_join_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ 
   const int64_t per = units_per_piece(*plan.units, plan.n_ctas);
   const int64_t u0 = plan.unit_start[gr] + ((int64_t)kvh * ((rows + kSharedTileRows - 1) / kSharedTileRows) + rt) * tiles;
   const int p0 = (int)(u0 / per), n = (int)((u0 + tiles - 1) / per) - p0 + 1;
-  const int64_t at = (int64_t)p0 * kSharedTileRows + (int64_t)(first - plan.group_ptr[0]) * a.n_kv_heads * a.group + (int64_t)kvh * rows + r;
+  // (an item of few rows has two parts in each piece, see pp_paged.h)
+  const int in_tile = r - rt * kSharedTileRows, item_rows = min(rows - rt * kSharedTileRows, kSharedTileRows), sides = item_rows <= kSharedTileRows / 2 ? 2 : 1;
+  const int64_t at = (int64_t)p0 * kSharedTileRows + plan.part_start[gr] + (int64_t)kvh * shared_part_rows(rows) + rt * kSharedTileRows + in_tile;
+  auto part_row = [&](int part) { return at + (int64_t)(sides == 2 ? part >> 1 : part) * kSharedTileRows + (sides == 2 && (part & 1) ? item_rows : 0); };
+  const int n_all = n * sides;
   float mm = kNoScore, ll = 0.f, oo[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) oo[e] = 0.f;
-  for (int base = 0; base < n; base += 32) {
-    const int here = min(32, n - base);
-    const float2 ml = lane < here ? plan.ml[at + (int64_t)(base + lane) * kSharedTileRows] : make_float2(kNoScore, 0.f);
-    float m_new = ml.x;
+  constexpr int kAtOnce = 8;            // parts whose loads are under way together
+  for (int base = 0; base < n_all; base += kAtOnce) {
+    float2 ml[kAtOnce];
+    float p[kAtOnce][E];
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) m_new = fmaxf(m_new, __shfl_xor_sync(0xffffffffu, m_new, o));
-    m_new = fmaxf(mm, m_new);
-    const float alpha = ex2(mm - m_new), f = ex2(ml.x - m_new);
+    for (int c = 0; c < kAtOnce; ++c) {
+      ml[c] = make_float2(kNoScore, 0.f);
+#pragma unroll
+      for (int e = 0; e < E; ++e) p[c][e] = 0.f;
+      if (base + c >= n_all) continue;
+      const int64_t from = part_row(base + c);
+      ml[c] = plan.ml[from];
+      const float* src = plan.o + from * D + E * lane;
+      if constexpr (E == 4) {
+        const float4 x = *reinterpret_cast<const float4*>(src);
+        p[c][0] = x.x; p[c][1] = x.y; p[c][2] = x.z; p[c][3] = x.w;
+      } else {
+        const float2 x = *reinterpret_cast<const float2*>(src);
+        p[c][0] = x.x; p[c][1] = x.y;
+      }
+    }
+    float m_new = mm;
+#pragma unroll
+    for (int c = 0; c < kAtOnce; ++c) m_new = fmaxf(m_new, ml[c].x);
+    const float alpha = ex2(mm - m_new);
     mm = m_new;
-    float l = ml.y * f;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
-    ll = ll * alpha + l;
+    ll *= alpha;
 #pragma unroll
     for (int e = 0; e < E; ++e) oo[e] *= alpha;
-#pragma unroll 8
-    for (int c = 0; c < here; ++c) {
-      const float fc = __shfl_sync(0xffffffffu, f, c);
-      const float* src = plan.o + (at + (int64_t)(base + c) * kSharedTileRows) * D + E * lane;
 #pragma unroll
-      for (int e = 0; e < E; ++e) oo[e] += src[e] * fc;
+    for (int c = 0; c < kAtOnce; ++c) {
+      if (ml[c].y == 0.f) continue;     // (a part that took no keys left no O)
+      const float f = ex2(ml[c].x - m_new);
+      ll += ml[c].y * f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) oo[e] += p[c][e] * f;
     }
   }
   if (lane == 0) plan.row_ml[row] = make_float2(mm, ll);
@@ -1376,6 +1398,7 @@ int decode_step(const pp_attn_params* params, const pp_paged_cache* cache, const
   if (n_groups > 0) {
     plan.units = reinterpret_cast<int64_t*>(ws + L.units);
     plan.unit_start = reinterpret_cast<int64_t*>(ws + L.unit_start);
+    plan.part_start = reinterpret_cast<int64_t*>(ws + L.part_start);
     plan.key_tiles = reinterpret_cast<int32_t*>(ws + L.key_tiles);
     plan.shared_rows = reinterpret_cast<int32_t*>(ws + L.shared_rows);
     plan.lead = reinterpret_cast<int32_t*>(ws + L.lead);
@@ -1427,13 +1450,14 @@ PagedWorkspace paged_workspace(const pp_attn_params& p, int32_t k, int32_t n_gro
   if (n_groups > 0) {
     L.units = take(sizeof(int64_t));
     L.unit_start = take(((size_t)n_groups + 1) * sizeof(int64_t));
+    L.part_start = take((size_t)n_groups * sizeof(int64_t));
     L.key_tiles = take((size_t)n_groups * sizeof(int32_t));
     L.shared_rows = take((size_t)n_groups * sizeof(int32_t));
     L.lead = take((size_t)n_groups * sizeof(int32_t));
     L.own_start = take((size_t)k * sizeof(int32_t));
     L.group_of = take((size_t)k * sizeof(int32_t));
     L.q_rot = take((size_t)k * p.n_q_heads * p.head_dim * sizeof(__nv_bfloat16));
-    const size_t rows = (size_t)kSms * kSharedTileRows + (size_t)k * p.n_q_heads;
+    const size_t rows = (size_t)kSms * kSharedTileRows + 2 * (size_t)k * p.n_q_heads;
     L.shared_ml = take(rows * sizeof(float2));
     L.shared_o = take(rows * p.head_dim * sizeof(float));
     L.row_ml = take((size_t)k * p.n_q_heads * sizeof(float2));

@@ -50,14 +50,16 @@ RopeAngles rope_angles(float base, int32_t head_dim);
 // Parts of results: (m, l), m in scaled log2 units, and the unnormalised sum of D floats for a query head.
 // Own rows: pp_paged.cu. Shared rows (a kernel over kSharedTileRows x kSharedTileKeys tiles): the work is a line of
 // units, one tile of keys against one tile of rows each, ordered by (group, KV head, row tile, key tile), and cut into equal
-// pieces, one for each CTA. CTA c's part of an item (group, KV head, row tile) lies at rows c * kSharedTileRows + (rows of all
-// items before it) of the arrays: pieces and items both only ascend, and an item has at most kSharedTileRows rows.
+// pieces, one for each CTA. CTA c's part of an item (group, KV head, row tile) lies at rows c * kSharedTileRows + (part rows of all
+// items before it) of the arrays: pieces and items both only ascend, and an item has at most kSharedTileRows part rows, one for each of
+// its rows, or two where it has so few rows that both tiles of the kernel work on them (first all those of one, then of the other).
 struct PagedWorkspace {
   size_t cut;                           // int4 for each piece of the line of own rows
   size_t part_ml, part_o;               // float2, float[D]
   // with shared rows only
   size_t units;                         // int64: units in all
   size_t unit_start;                    // int64 [n_groups + 1]
+  size_t part_start;                    // int64 [n_groups]: part rows before the group's
   size_t key_tiles;                     // int32 [n_groups]
   size_t shared_rows;                   // int32 [n_groups]: rows of pages read for the group
   size_t lead;                          // int32 [n_groups]: the prompt whose row of the page table stands for the group's
@@ -73,7 +75,7 @@ PagedWorkspace paged_workspace(const pp_attn_params& p, int32_t k, int32_t n_gro
 // The plan of the shared rows as the kernels find it in the workspace.
 struct SharedPlan {
   int64_t* units;
-  int64_t* unit_start;
+  int64_t *unit_start, *part_start;
   int32_t *key_tiles, *shared_rows, *lead, *own_start, *group_of;
   __nv_bfloat16* q_rot;
   float2 *ml, *row_ml;
@@ -88,6 +90,11 @@ int launch_shared_attention(const pp_attn_params& p, const PagedCacheArgs& c, co
 #ifdef __CUDACC__
 // Units of each piece.
 __device__ __forceinline__ int64_t units_per_piece(int64_t units, int32_t n_ctas) { return (units + n_ctas - 1) / n_ctas; }
+// Part rows of a group and KV head with so many query rows.
+__device__ __forceinline__ int shared_part_rows(int rows) {
+  const int last = rows % kSharedTileRows;
+  return rows + (last <= kSharedTileRows / 2 ? last : 0);
+}
 #endif
 
 }  // namespace pp

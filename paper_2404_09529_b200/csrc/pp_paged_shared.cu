@@ -11,7 +11,8 @@
 //   warps 2-3    TMA-load Q of tile 0 / 1
 //   warps 4-7    softmax of tile 0, a thread per row: no row is split between threads, so nothing is exchanged
 //   warps 8-11   the same for tile 1
-// A tile's softmax runs while the other tile's products do. The pages of a tile that the group does not share are loaded from
+// A tile's softmax runs while the other tile's products do. An item of at most 128 rows has no second row tile: the two then take its
+// key tiles in turn, each with an O of its own, so that there are two chains of product, softmax and product here too. The pages of a tile that the group does not share are loaded from
 // beyond the last page, which TMA fills with zeros.
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -146,7 +147,6 @@ shared_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
       const int mine = lane / kChunks, chunk = lane - mine * kChunks;
       const uint32_t lane_issue = lane < boxes ? 1u : 0u;
       const uint32_t lane_dst = (uint32_t)(chunk * BN + mine * box_rows) * 128u;
-      const int first_prompt = plan.group_ptr[0];
       uint32_t it_n = 0, stage = 0, phase = 0;
       bool ok = true;
       for (int64_t u = (int64_t)blockIdx.x * per;; ) {
@@ -172,8 +172,7 @@ shared_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
         const int kv_head = item / row_tiles, rt = item - kv_head * row_tiles;
         const int n = (int)min((int64_t)(tiles - tile0), u_end - u);
         const int rows_here = min(rows - rt * kSharedTileRows, kSharedTileRows), shared = plan.shared_rows[gr];
-        const int64_t out = (int64_t)blockIdx.x * kSharedTileRows + (int64_t)(first - first_prompt) * args.n_kv_heads * args.group +
-                            (int64_t)kv_head * rows + rt * kSharedTileRows;
+        const int64_t out = (int64_t)blockIdx.x * kSharedTileRows + plan.part_start[gr] + (int64_t)kv_head * shared_part_rows(rows) + rt * kSharedTileRows;
         if (issue) {
           e[0] = n;
           e[1] = rows_here;
@@ -219,35 +218,46 @@ shared_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
       const uint32_t issue = elect_one();
       uint32_t it_n = 0, kv = 0, count[2] = {0, 0};       // kv: K and V tiles of the items before (K of tile j: kv + 2j)
       int n = 0;
-      bool used1 = false, ok = true;
+      bool split = false, ok = true;
       auto wait_kv = [&](uint32_t at) { return mbar_wait_issuer<kWaitKvFull>(bar_kv_full + 8 * (at % NS), (at / NS) & 1u, wctx); };
+      // The scores are what a tile's softmax waits for: their commit comes first, the one that gives the stages back after it.
       auto issue_qk = [&](int t, int j) {
         const uint32_t s = (kv + 2u * (uint32_t)j) % NS;
         tc_fence_after();
-        const uint32_t a = q_lo + (uint32_t)t * (Cfg::kQBytes >> 4), b = k_lo + s * (Cfg::kTileBytes >> 4);
+        const uint32_t a = q_lo + (split ? 0u : (uint32_t)t) * (Cfg::kQBytes >> 4), b = k_lo + s * (Cfg::kTileBytes >> 4);
 #pragma unroll
         for (int kk = 0; kk < D / 16; ++kk)
           mma_ss(tmem_base + 128u * t, a + (uint32_t)(kk >> 2) * ((BM * 128) >> 4) + (uint32_t)(kk & 3) * 2,
                  b + (uint32_t)(kk >> 2) * ((BN * 128) >> 4) + (uint32_t)(kk & 3) * 2, idesc_qk, kk > 0 ? 1u : 0u, issue);
-        if (t == 1 || !used1) tc_commit(bar_kv_empty + 8 * s, issue);
         tc_commit(bar_s_full + 8 * t, issue);
-        if (j + 1 == n) tc_commit(bar_q_empty + 8 * t, issue);
+        if (t == 1 || split) tc_commit(bar_kv_empty + 8 * s, issue);
+        if (j + 1 == n) tc_commit(bar_q_empty + (split ? 0 : 8 * t), issue);
       };
-      auto step = [&](int t, int j) -> bool {
-        if (j == 0 && !mbar_wait_issuer<kWaitOEmpty>(bar_o_empty + 8 * t, (it_n & 1u) ^ 1u, wctx)) return false;
-        const uint32_t vc = kv + 2u * (uint32_t)j + 1u, s = vc % NS;
+      // O_t (+)= P_t V_j, then the tile's next scores, those of key tile `next`. The next K is waited for first where it has been there
+      // for long (both row tiles read it); of an item that is split it may be the one that is loaded last.
+      auto step = [&](int t, int j, bool first, int next) -> bool {
+        if (first && !mbar_wait_issuer<kWaitOEmpty>(bar_o_empty + 8 * t, (it_n & 1u) ^ 1u, wctx)) return false;
+        const uint32_t vc = kv + 2u * (uint32_t)j + 1u, s = vc % NS, kc = kv + 2u * (uint32_t)next;
         if (!wait_kv(vc)) return false;
-        if (j + 1 < n && !wait_kv(vc + 1u)) return false;
+        if (!split && next < n && !wait_kv(kc)) return false;
         if (!mbar_wait_issuer<kWaitP>(bar_p_full + 8 * t, count[t] & 1u, wctx)) return false;
         tc_fence_after();
         const uint32_t d = tmem_base + 256u + (uint32_t)(D * t), a = tmem_base + 128u * t, b = v_lo + s * (Cfg::kTileBytes >> 4);
 #pragma unroll
         for (int kk = 0; kk < BN / 16; ++kk)
-          mma_ts(d, a + kk * 8, b + (uint32_t)kk * ((16 * 128) >> 4), idesc_pv, kk > 0 || j > 0 ? 1u : 0u, issue);
+          mma_ts(d, a + kk * 8, b + (uint32_t)kk * ((16 * 128) >> 4), idesc_pv, kk > 0 || !first ? 1u : 0u, issue);
         ++count[t];
-        if (t == 1 || !used1) tc_commit(bar_kv_empty + 8 * s, issue);
-        if (j + 1 < n) issue_qk(t, j + 1);
-        else tc_commit(bar_o_full + 8 * t, issue);
+        if (next < n) {
+          if (split) {
+            tc_commit(bar_kv_empty + 8 * s, issue);
+            if (!wait_kv(kc)) return false;
+          }
+          issue_qk(t, next);
+          if (!split && t == 1) tc_commit(bar_kv_empty + 8 * s, issue);
+        } else {
+          if (t == 1 || split) tc_commit(bar_kv_empty + 8 * s, issue);
+          tc_commit(bar_o_full + 8 * t, issue);
+        }
         return true;
       };
       while (ok) {
@@ -255,28 +265,31 @@ shared_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
         if (!mbar_wait_issuer<kWaitItemFull>(bar_item_full + 8 * ring, (it_n / kRing) & 1u, wctx)) break;
         const volatile int* e = s_ring + ring * kRingInts;
         n = uniform(e[0]);
-        used1 = uniform(e[1]) > BM;
+        split = uniform(e[1]) <= BM;
         if (issue) mbar_arrive(bar_item_empty + 8 * ring);
         if (n < 0) break;
         if (!(ok = mbar_wait_issuer<kWaitQFull>(bar_q_full, it_n & 1u, wctx) && mbar_wait_issuer<kWaitQFull>(bar_q_full + 8, it_n & 1u, wctx) &&
                    wait_kv(kv)))
           break;
         issue_qk(0, 0);
-        if (used1) issue_qk(1, 0);
-        for (int j = 0; ok && j < n; ++j) {
-          ok = step(0, j);
-          if (ok && used1) ok = step(1, j);
+        if (!split) {
+          issue_qk(1, 0);
+          for (int j = 0; ok && j < n; ++j) ok = step(0, j, j == 0, j + 1) && step(1, j, j == 0, j + 1);
+        } else {
+          if (n > 1) {
+            if (!(ok = wait_kv(kv + 2u))) break;
+            issue_qk(1, 1);
+          }
+          for (int j = 0; ok && j < n; ++j) ok = step(j & 1, j, j < 2, j + 2);
+          if (ok && n == 1) {
+            // Tile 1 has nothing, but keeps its barriers in step, one phase for each item; all of its softmax threads must have seen
+            // the phase before.
+            if (!(ok = mbar_wait_issuer<kWaitOEmpty>(bar_o_empty + 8, (it_n & 1u) ^ 1u, wctx))) break;
+            if (issue) mbar_arrive(bar_o_full + 8);
+          }
+          if (ok && issue) mbar_arrive(bar_q_empty + 8);       // (no query was loaded for it)
         }
         if (!ok) break;
-        if (!used1) {
-          // The unused tile keeps its barriers in step, one phase for each item; all of its softmax threads must have seen the
-          // phase before.
-          if (!(ok = mbar_wait_issuer<kWaitOEmpty>(bar_o_empty + 8, (it_n & 1u) ^ 1u, wctx))) break;
-          if (issue) {
-            mbar_arrive(bar_q_empty + 8);
-            mbar_arrive(bar_o_full + 8);
-          }
-        }
         kv += 2u * (uint32_t)n;
         ++it_n;
       }
@@ -313,15 +326,24 @@ shared_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
       const uint32_t ring = it_n % kRing;
       if (!mbar_wait_warp<kWaitItemFull>(bar_item_full + 8 * ring, (it_n / kRing) & 1u, wctx)) break;
       const volatile int* e = s_ring + ring * kRingInts;
-      const int n = uniform(e[0]), rows = uniform(e[1]) - BM * t, last_keys = uniform(e[4]);
-      const int64_t out = (int64_t)((uint64_t)(uint32_t)uniform(e[5]) | ((uint64_t)(uint32_t)uniform(e[6]) << 32)) + BM * t;
+      const int n = uniform(e[0]), item_rows = uniform(e[1]), last_keys = uniform(e[4]);
+      const bool split = item_rows <= BM;
+      const int rows = split ? item_rows : item_rows - BM * t;            // of this tile
+      const int64_t out = (int64_t)((uint64_t)(uint32_t)uniform(e[5]) | ((uint64_t)(uint32_t)uniform(e[6]) << 32)) + (split ? item_rows : BM) * t;
       if (lane == 0) mbar_arrive(bar_item_empty + 8 * ring);
       if (n < 0) break;
       float m_run = -INFINITY, neg_m = 0.f;
       uint64_t sum_a = 0ull, sum_b = 0ull;
       bool ok = true;
-      for (int j = 0; rows > 0 && j < n; ++j) {
+      const bool idle = 32 * quad >= rows;        // a warp without rows leaves its P as it is: no other row reads it
+      const int first = split ? t : 0, each = split ? 2 : 1;
+      for (int j = first; j < n; j += each) {
         if (!(ok = mbar_wait_warp<kWaitS>(bar_s_full + 8 * t, count & 1u, wctx))) break;
+        if (idle) {
+          mbar_arrive(bar_p_full + 8 * t);
+          ++count;
+          continue;
+        }
         tc_fence_after();
         uint32_t v[BN];
 #pragma unroll
@@ -334,7 +356,7 @@ shared_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
         const float m_tile = fmaxf(max64(*reinterpret_cast<uint32_t(*)[64]>(&v[0])), max64(*reinterpret_cast<uint32_t(*)[64]>(&v[64]))) * c_scale;
         const float m_new = m_tile > m_run + kLazyLog2 ? m_tile : m_run;
         const bool rescale = m_new != m_run && m_run != -INFINITY;
-        if (j > 0 && __any_sync(0xffffffffu, rescale)) {
+        if (j != first && __any_sync(0xffffffffu, rescale)) {
           // (these scores are there, so the product before them, P V of the tile before, is done)
           const float alpha = rescale ? fast_exp2(m_run - m_new) : 1.f;
 #pragma unroll 1
@@ -366,12 +388,13 @@ shared_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
       }
       if (!ok) break;
       if (!mbar_wait_warp<kWaitOFull>(bar_o_full + 8 * t, it_n & 1u, wctx)) break;
-      if (rows > 0) {
+      if (!idle) {
         tc_fence_after();
+        const bool any = first < n;               // (a tile that took no keys leaves l = 0, and its O is not looked at)
         if (row < rows) args.plan.ml[out + row] = make_float2(fmaxf(m_run, -FLT_MAX), sum_f2x2(sum_a, sum_b));
         float4* dst = reinterpret_cast<float4*>(args.plan.o + (out + row) * D);
 #pragma unroll 1
-        for (int ch = 0; ch < D / 32; ++ch) {
+        for (int ch = 0; any && ch < D / 32; ++ch) {
           uint32_t ov[32];
           tmem_ld32(tm_o + 32 * ch, ov);
           tc_wait_ld();
