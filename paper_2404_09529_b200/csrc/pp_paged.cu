@@ -220,7 +220,7 @@ enum WaitCode { kWaitRows = 41 };
 struct PagedArgs {
   PagedCacheArgs c;
   const int32_t* lengths;
-  const int32_t* own_start;             // rows before it are read by the kernel of the shared rows; null: none are
+  const int2* own;                      // .x: rows before it are read by the kernel of the shared rows; null: none are
   const __nv_bfloat16 *q_new, *k_new, *v_new;
   int64_t q_stride, k_stride, v_stride;
   __nv_bfloat16* o;
@@ -412,6 +412,12 @@ struct Rows<D, false> {
   }
   // element of O that acc[j][0], acc[j][1] (x = 0) and acc[j][2], acc[j][3] (x = 1) stand for
   static __device__ __forceinline__ int element(int j, int x, int g) { return 16 * j + 8 * x + g; }
+  // and at place (D / 8) g + 2 j + x of a part, so that those of a lane stand together
+  static __device__ __forceinline__ int element_at(int place) {
+    const int g = place / (D / 8), r = place % (D / 8);
+    return 16 * (r >> 1) + 8 * (r & 1) + g;
+  }
+  static __device__ __forceinline__ int place_of(int element) { return (D / 8) * (element & 7) + (element >> 4) * 2 + ((element >> 3) & 1); }
   // O of the eight heads as rows of bf16, heads 2t and 2t + 1 times f0 and f1 (transposed, a lane holds pairs of elements of one head)
   static __device__ __forceinline__ void leave(const float (&acc)[D / 16][4], float f0, float f1, uint32_t at, int g, int t) {
 #pragma unroll
@@ -535,6 +541,7 @@ struct Rows<D, true> {
     }
   }
   static __device__ __forceinline__ int element(int j, int x, int g) { return (D / 8) * g + 2 * j + x; }
+  static __device__ __forceinline__ int element_at(int place) { return place; }
   static __device__ __forceinline__ void leave(const float (&acc)[D / 16][4], float f0, float f1, uint32_t at, int g, int t) {
 #pragma unroll
     for (int j = 0; j < D / 16; ++j)
@@ -576,7 +583,7 @@ struct Line {
     start = 0;
     if (i < a.n_prompts) {
       len = checked_length(a.c, a.lengths, i, fresh, nullptr);
-      if (a.own_start) start = a.own_start[i];
+      if (a.own) start = a.own[i].x;
     }
   }
   __device__ __forceinline__ int64_t line_units(int len, int start) const { return (int64_t)(units(len, start) + kItemUnits) * a.n_kv_heads; }
@@ -644,7 +651,7 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
   int64_t mine = 0, total;
   for (int i = tid * each; i < min((tid + 1) * each, a.n_prompts); ++i) {
     const int len = checked_length(a.c, a.lengths, i, fresh, blockIdx.x == 0 ? a.status : nullptr);
-    if (len >= 0) mine += line.line_units(len, a.own_start ? a.own_start[i] : 0);
+    if (len >= 0) mine += line.line_units(len, a.own ? a.own[i].x : 0);
   }
   s_before[tid] = block_prefix<kThreads>(mine, s_warp, total);
   __syncthreads();
@@ -774,10 +781,13 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
         const float2 ml = plan.row_ml[at];
         m[h] = ml.x;
         l[h] = g == 0 ? ml.y : 0.f;
+        const float4* from = reinterpret_cast<const float4*>(plan.row_o + at * D + (D / 8) * g);
 #pragma unroll
-        for (int j = 0; j < D / 16; ++j)
-#pragma unroll
-          for (int x = 0; x < 2; ++x) acc[j][2 * x + h] = plan.row_o[at * D + R::element(j, x, g)];
+        for (int j = 0; j < D / 16; j += 2) {
+          const float4 x = from[j >> 1];
+          acc[j][h] = x.x; acc[j][2 + h] = x.y;
+          acc[j + 1][h] = x.z; acc[j + 1][2 + h] = x.w;
+        }
       }
     }
     if (angles_of != c.i) {
@@ -972,11 +982,10 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
         const int head = 2 * t + h;
         if (head >= a.group) continue;
         if (g == 0) a.part_ml[slot * a.group + head] = make_float2(m[h], l[h]);
-        float* to = a.part_o + (slot * a.group + head) * D;
+        float4* to = reinterpret_cast<float4*>(a.part_o + (slot * a.group + head) * D + (D / 8) * g);
 #pragma unroll
-        for (int j = 0; j < D / 16; ++j)
-#pragma unroll
-          for (int x = 0; x < 2; ++x) to[R::element(j, x, g)] = acc[j][2 * x + h] * out_scale;
+        for (int j = 0; j < D / 16; j += 2)
+          to[j >> 1] = make_float4(acc[j][h] * out_scale, acc[j][2 + h] * out_scale, acc[j + 1][h] * out_scale, acc[j + 1][2 + h] * out_scale);
       }
       if (begins && lane == 0)          // the pieces over which the item goes on: units behind this one's end
         a.cut[piece] = make_int4(c.i, c.kvh, 1 + (int)((c.units - c.n + per - 1) / per), 0);
@@ -986,38 +995,28 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
   }
 }
 
-// Joins the parts of the items that are cut: a CTA for a query head of the KV head and a piece in which such an item may begin (the
-// others leave at once). Its warps share the parts: one prompt alone may have hundreds.
+// The parts of one query head, (m, l) and D floats each, joined by one warp: parts first, first + step, ... of n; `at` says where a part lies.
 template <int D>
-__global__ void __launch_bounds__(kCombineThreads)
-paged_combine_kernel(const __grid_constant__ PagedArgs a) {
-  constexpr int E = D / 32, kWarps = kCombineThreads / 32;      // E: consecutive elements per lane
-  __shared__ float s_m[kWarps], s_l[kWarps], s_o[kWarps][D];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, h = blockIdx.y;
-  pdl_wait();                           // the parts come from the kernels before this one
-  pdl_launch_dependents();
-  const int piece = blockIdx.x;
-  const int4 cut = a.cut[piece];
-  if (cut.z == 0) return;
-  float mm = kNoScore, ll = 0.f, oo[E];
-#pragma unroll
-  for (int e = 0; e < E; ++e) oo[e] = 0.f;
-  const int n_all = cut.z;
-  const int64_t first = 2 * (int64_t)piece;
-  auto slot = [&](int part) { return (first + (part == 0 ? 1 : 2 * part)) * a.group + h; };
-  constexpr int kAtOnce = 4;          // parts whose loads are under way together
-  for (int base = warp; base < n_all; base += kAtOnce * kWarps) {
+struct Joined {
+  static constexpr int E = D / 32;      // consecutive elements per lane
+  float m, l, o[E];
+};
+template <int D, int kAtOnce, class At>
+__device__ __forceinline__ Joined<D> join_parts(int first, int step, int n, const float2* mls, const float* os, int lane, const At& at) {
+  constexpr int E = D / 32;
+  Joined<D> s{kNoScore, 0.f, {}};
+  for (int base = first; base < n; base += kAtOnce * step) {
     float2 ml[kAtOnce];
     float p[kAtOnce][E];
 #pragma unroll
-    for (int c = 0; c < kAtOnce; ++c) {
+    for (int c = 0; c < kAtOnce; ++c) {               // (all of these loads are under way together)
       ml[c] = make_float2(kNoScore, 0.f);
 #pragma unroll
       for (int e = 0; e < E; ++e) p[c][e] = 0.f;
-      if (base + c * kWarps >= n_all) continue;
-      const int64_t at = slot(base + c * kWarps);
-      ml[c] = a.part_ml[at];
-      const float* src = a.part_o + at * D + E * lane;
+      if (base + c * step >= n) continue;
+      const int64_t from = at(base + c * step);
+      ml[c] = mls[from];
+      const float* src = os + from * D + E * lane;
       if constexpr (E == 4) {
         const float4 x = *reinterpret_cast<const float4*>(src);
         p[c][0] = x.x; p[c][1] = x.y; p[c][2] = x.z; p[c][3] = x.w;
@@ -1026,40 +1025,85 @@ paged_combine_kernel(const __grid_constant__ PagedArgs a) {
         p[c][0] = x.x; p[c][1] = x.y;
       }
     }
-    float m_new = mm;
+    float m_new = s.m;
 #pragma unroll
     for (int c = 0; c < kAtOnce; ++c) m_new = fmaxf(m_new, ml[c].x);
-    const float alpha = ex2(mm - m_new);
-    mm = m_new;
-    ll *= alpha;
+    const float alpha = ex2(s.m - m_new);
+    s.m = m_new;
+    s.l *= alpha;
 #pragma unroll
-    for (int e = 0; e < E; ++e) oo[e] *= alpha;
+    for (int e = 0; e < E; ++e) s.o[e] *= alpha;
 #pragma unroll
     for (int c = 0; c < kAtOnce; ++c) {
+      if (ml[c].y == 0.f) continue;     // (a part that took no keys may have left no O)
       const float f = ex2(ml[c].x - m_new);
-      ll += ml[c].y * f;
+      s.l += ml[c].y * f;
 #pragma unroll
-      for (int e = 0; e < E; ++e) oo[e] += p[c][e] * f;
+      for (int e = 0; e < E; ++e) s.o[e] += p[c][e] * f;
     }
   }
-  if (lane == 0) { s_m[warp] = mm; s_l[warp] = ll; }
+  return s;
+}
+// What the warps of a CTA have joined of one head, as one; the result is warp 0's. (Ends with a barrier.)
+template <int D, int kWarps>
+struct JoinSpace { float m[kWarps], l[kWarps], o[kWarps][D]; };
+template <int D, int kWarps>
+__device__ __forceinline__ void join_warps(Joined<D>& s, JoinSpace<D, kWarps>& space, int warp, int lane) {
+  constexpr int E = D / 32;
+  if (lane == 0) {
+    space.m[warp] = s.m;
+    space.l[warp] = s.l;
+  }
 #pragma unroll
-  for (int e = 0; e < E; ++e) s_o[warp][E * lane + e] = oo[e];
+  for (int e = 0; e < E; ++e) space.o[warp][E * lane + e] = s.o[e];
   __syncthreads();
-  if (threadIdx.x < D) {
-    mm = s_m[0];
+  if (warp == 0) {
+    float m = space.m[0];
 #pragma unroll
-    for (int w = 1; w < kWarps; ++w) mm = fmaxf(mm, s_m[w]);
-    ll = 0.f;
-    float o = 0.f;
+    for (int w = 1; w < kWarps; ++w) m = fmaxf(m, space.m[w]);
+    s = Joined<D>{m, 0.f, {}};
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) {
-      const float f = ex2(s_m[w] - mm);
-      ll += s_l[w] * f;
-      o += s_o[w][threadIdx.x] * f;
+      if (space.l[w] == 0.f) continue;
+      const float f = ex2(space.m[w] - m);
+      s.l += space.l[w] * f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) s.o[e] += space.o[w][E * lane + e] * f;
     }
-    // (an item that is cut has rows)
-    a.o[((int64_t)cut.x * a.n_q_heads + cut.y * a.group + h) * D + threadIdx.x] = __float2bfloat16_rn(o / ll);
+  }
+  __syncthreads();
+}
+
+// Joins the parts of the items that are cut: a warp for a query head and a piece in which such an item may begin (neighbouring warps:
+// neighbouring pieces). An item in many parts (one prompt alone may have a hundred) is the work of the whole CTA.
+template <int D, class R>
+__global__ void __launch_bounds__(kCombineThreads)
+paged_combine_kernel(const __grid_constant__ PagedArgs a, int n_pieces) {
+  constexpr int E = D / 32, kWarps = kCombineThreads / 32, kManyParts = 12;
+  __shared__ JoinSpace<D, kWarps> space;
+  __shared__ int4 s_cut[kWarps];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  pdl_wait();                           // the parts come from the kernels before this one
+  pdl_launch_dependents();
+  const int h = blockIdx.y, piece0 = blockIdx.x * kWarps, piece = piece0 + warp;
+  const int4 cut = piece < n_pieces ? a.cut[piece] : make_int4(0, 0, 0, 0);
+  auto leave = [&](const int4& c, const Joined<D>& s) {         // (an item that is cut has rows)
+    __nv_bfloat16* to = a.o + ((int64_t)c.x * a.n_q_heads + c.y * a.group + h) * D;
+#pragma unroll
+    for (int e = 0; e < E; ++e) to[R::element_at(E * lane + e)] = __float2bfloat16_rn(s.o[e] / s.l);
+  };
+  auto at = [&](int first) { return [first, h, group = a.group](int part) { return (2 * (int64_t)first + (part == 0 ? 1 : 2 * part)) * group + h; }; };
+  const bool many = cut.z > kManyParts;
+  if (cut.z > 0 && !many) leave(cut, join_parts<D, 4>(0, 1, cut.z, a.part_ml, a.part_o, lane, at(piece)));
+  if (!__syncthreads_or(many)) return;
+  if (lane == 0) s_cut[warp] = many ? cut : make_int4(0, 0, 0, 0);
+  __syncthreads();
+  for (int w = 0; w < kWarps; ++w) {
+    const int4 c = s_cut[w];
+    if (c.z == 0) continue;
+    Joined<D> s = join_parts<D, 4>(warp, kWarps, c.z, a.part_ml, a.part_o, lane, at(piece0 + w));
+    join_warps<D, kWarps>(s, space, warp, lane);
+    if (warp == 0) leave(c, s);
   }
 }
 
@@ -1139,7 +1183,6 @@ shared_plan_kernel(const __grid_constant__ PlanArgs p) {
   };
   for (int i = tid; i < k; i += kPlanThreads) {
     const int g = group_of(i), len = checked_length(a.c, a.lengths, i, fresh, nullptr);
-    plan.group_of[i] = g;
     if (g >= 0 && len >= 0) {
       atomicMin(&s_rows[g], len);
       atomicMin(&s_lead[g], i);
@@ -1159,93 +1202,61 @@ shared_plan_kernel(const __grid_constant__ PlanArgs p) {
   }
   int64_t all, none, at = block_prefix<kPlanThreads>(units, s_warp, all), part = block_prefix<kPlanThreads>(parts, s_warp, none);
   for (int g = g0; g < g1; ++g) {
-    const int prompts = bad ? 0 : s_ptr[g + 1] - s_ptr[g], tiles = (s_rows[g] + kSharedTileKeys - 1) / kSharedTileKeys;
-    plan.unit_start[g] = at;
-    plan.part_start[g] = part;
-    plan.key_tiles[g] = tiles;
-    plan.shared_rows[g] = s_rows[g];
-    plan.lead[g] = s_lead[g];
-    at += (int64_t)tiles * ((prompts * a.group + kSharedTileRows - 1) / kSharedTileRows) * a.n_kv_heads;
-    part += (int64_t)shared_part_rows(prompts * a.group) * a.n_kv_heads;
+    const int prompts = bad ? 0 : s_ptr[g + 1] - s_ptr[g];
+    SharedGroup x;
+    x.unit_start = at;
+    x.part_start = part;
+    x.key_tiles = (s_rows[g] + kSharedTileKeys - 1) / kSharedTileKeys;
+    x.shared_rows = s_rows[g];
+    x.lead = s_lead[g];
+    x.first = s_ptr[g];
+    x.query_rows = prompts * a.group;
+    plan.groups[g] = x;
+    at += (int64_t)x.key_tiles * ((x.query_rows + kSharedTileRows - 1) / kSharedTileRows) * a.n_kv_heads;
+    part += (int64_t)shared_part_rows(x.query_rows) * a.n_kv_heads;
   }
-  if (tid == 0) {
-    plan.unit_start[n] = all;
-    *plan.units = all;
-  }
+  if (tid == 0) *plan.units = all;
   __syncthreads();
   for (int i = tid; i < k; i += kPlanThreads) {
     const int g = group_of(i);
-    plan.own_start[i] = g >= 0 && a.lengths[i] >= 0 ? s_rows[g] : 0;
+    plan.prompts[i] = make_int2(g >= 0 && a.lengths[i] >= 0 ? s_rows[g] : 0, g);
   }
 }
 
-// The parts of every query head over the shared rows, from the CTAs of the attention kernel, become one: a warp for each head of
-// each prompt. The step over the prompts' own rows goes on from there.
-template <int D>
+// The parts of every query head over the shared rows, from the CTAs of the attention kernel, become one: a warp for each head of each
+// prompt, or, of few, a CTA (kAcross). The step over the prompts' own rows goes on from there, and finds the elements in its order.
+template <int D, bool kAcross>
 __global__ void __launch_bounds__(kCombineThreads)
 shared_join_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ SharedPlan plan) {
-  constexpr int E = D / 32;
-  const int lane = threadIdx.x & 31;
-  const int64_t row = (int64_t)blockIdx.x * (kCombineThreads / 32) + (threadIdx.x >> 5);
+  using R = Rows<D, false>;
+  constexpr int E = D / 32, kWarps = kCombineThreads / 32;
+  __shared__ JoinSpace<D, kAcross ? kWarps : 1> space;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int64_t row = kAcross ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * kWarps + warp;
   pdl_wait();
   pdl_launch_dependents();
   if (row >= (int64_t)a.n_prompts * a.n_q_heads) return;
   const int i = (int)(row / a.n_q_heads), head = (int)(row - (int64_t)i * a.n_q_heads), kvh = head / a.group;
-  if (plan.own_start[i] == 0) return;   // nothing shared
-  const int gr = plan.group_of[i], tiles = plan.key_tiles[gr], first = plan.group_ptr[gr], rows = (plan.group_ptr[gr + 1] - first) * a.group;
-  const int r = (i - first) * a.group + head - kvh * a.group, rt = r / kSharedTileRows;
+  const int2 own = plan.prompts[i];
   const int64_t per = units_per_piece(*plan.units, plan.n_ctas);
-  const int64_t u0 = plan.unit_start[gr] + ((int64_t)kvh * ((rows + kSharedTileRows - 1) / kSharedTileRows) + rt) * tiles;
-  const int p0 = (int)(u0 / per), n = (int)((u0 + tiles - 1) / per) - p0 + 1;
+  if (own.x == 0) return;               // nothing shared
+  const SharedGroup gr = plan.groups[own.y];
+  const int r = (i - gr.first) * a.group + head - kvh * a.group, rt = r / kSharedTileRows;
+  const int64_t u0 = gr.unit_start + ((int64_t)kvh * ((gr.query_rows + kSharedTileRows - 1) / kSharedTileRows) + rt) * gr.key_tiles;
+  const int p0 = (int)(u0 / per), n = (int)((u0 + gr.key_tiles - 1) / per) - p0 + 1;
   // (an item of few rows has two parts in each piece, see pp_paged.h)
-  const int in_tile = r - rt * kSharedTileRows, item_rows = min(rows - rt * kSharedTileRows, kSharedTileRows), sides = item_rows <= kSharedTileRows / 2 ? 2 : 1;
-  const int64_t at = (int64_t)p0 * kSharedTileRows + plan.part_start[gr] + (int64_t)kvh * shared_part_rows(rows) + rt * kSharedTileRows + in_tile;
+  const int item_rows = min(gr.query_rows - rt * kSharedTileRows, kSharedTileRows), sides = item_rows <= kSharedTileRows / 2 ? 2 : 1;
+  const int64_t at = (int64_t)p0 * kSharedTileRows + gr.part_start + (int64_t)kvh * shared_part_rows(gr.query_rows) + r;
   auto part_row = [&](int part) { return at + (int64_t)(sides == 2 ? part >> 1 : part) * kSharedTileRows + (sides == 2 && (part & 1) ? item_rows : 0); };
-  const int n_all = n * sides;
-  float mm = kNoScore, ll = 0.f, oo[E];
-#pragma unroll
-  for (int e = 0; e < E; ++e) oo[e] = 0.f;
-  constexpr int kAtOnce = 8;            // parts whose loads are under way together
-  for (int base = 0; base < n_all; base += kAtOnce) {
-    float2 ml[kAtOnce];
-    float p[kAtOnce][E];
-#pragma unroll
-    for (int c = 0; c < kAtOnce; ++c) {
-      ml[c] = make_float2(kNoScore, 0.f);
-#pragma unroll
-      for (int e = 0; e < E; ++e) p[c][e] = 0.f;
-      if (base + c >= n_all) continue;
-      const int64_t from = part_row(base + c);
-      ml[c] = plan.ml[from];
-      const float* src = plan.o + from * D + E * lane;
-      if constexpr (E == 4) {
-        const float4 x = *reinterpret_cast<const float4*>(src);
-        p[c][0] = x.x; p[c][1] = x.y; p[c][2] = x.z; p[c][3] = x.w;
-      } else {
-        const float2 x = *reinterpret_cast<const float2*>(src);
-        p[c][0] = x.x; p[c][1] = x.y;
-      }
-    }
-    float m_new = mm;
-#pragma unroll
-    for (int c = 0; c < kAtOnce; ++c) m_new = fmaxf(m_new, ml[c].x);
-    const float alpha = ex2(mm - m_new);
-    mm = m_new;
-    ll *= alpha;
-#pragma unroll
-    for (int e = 0; e < E; ++e) oo[e] *= alpha;
-#pragma unroll
-    for (int c = 0; c < kAtOnce; ++c) {
-      if (ml[c].y == 0.f) continue;     // (a part that took no keys left no O)
-      const float f = ex2(ml[c].x - m_new);
-      ll += ml[c].y * f;
-#pragma unroll
-      for (int e = 0; e < E; ++e) oo[e] += p[c][e] * f;
-    }
+  Joined<D> s = kAcross ? join_parts<D, 4>(warp, kWarps, n * sides, plan.ml, plan.o, lane, part_row)
+                        : join_parts<D, 4>(0, 1, n * sides, plan.ml, plan.o, lane, part_row);
+  if constexpr (kAcross) {
+    join_warps<D, kWarps>(s, space, warp, lane);
+    if (warp != 0) return;
   }
-  if (lane == 0) plan.row_ml[row] = make_float2(mm, ll);
+  if (lane == 0) plan.row_ml[row] = make_float2(s.m, s.l);
 #pragma unroll
-  for (int e = 0; e < E; ++e) plan.row_o[row * D + E * lane + e] = oo[e];
+  for (int e = 0; e < E; ++e) plan.row_o[row * D + R::place_of(E * lane + e)] = s.o[e];
 }
 
 // ------------------------------------------------------------------------------------------
@@ -1334,7 +1345,7 @@ cudaError_t launch_paged_decode(const PagedArgs& a, const SharedPlan& plan, cuda
   if (!page_map(&mk, a.c.k_pages, a, D, kE4m3) || !page_map(&mv, a.c.v_pages, a, D, kE4m3)) return cudaErrorInvalidValue;
   e = launch_dependent(paged_decode_kernel<D, kE4m3>, dim3(kSms), dim3(32 * kWarps), (size_t)kSmem, s, mk, mv, a, plan);
   if (e != cudaSuccess) return e;
-  return launch_dependent(paged_combine_kernel<D>, dim3(kSms * kWarps, a.group), dim3(kCombineThreads), 0, s, a);
+  return launch_dependent(paged_combine_kernel<D, Rows<D, kE4m3>>, dim3((kSms * kWarps + kCombineThreads / 32 - 1) / (kCombineThreads / 32), a.group), dim3(kCombineThreads), 0, s, a, kSms * kWarps);
 }
 
 template <int D>
@@ -1377,7 +1388,7 @@ int decode_step(const pp_attn_params* params, const pp_paged_cache* cache, const
   char* ws = static_cast<char*>(workspace);
   a.c = paged_cache_args(*cache);
   a.lengths = lengths;
-  a.own_start = n_groups > 0 ? reinterpret_cast<const int32_t*>(ws + L.own_start) : nullptr;
+  a.own = n_groups > 0 ? reinterpret_cast<const int2*>(ws + L.prompts) : nullptr;
   a.q_new = static_cast<const __nv_bfloat16*>(q_new);
   a.k_new = static_cast<const __nv_bfloat16*>(k_new);
   a.v_new = static_cast<const __nv_bfloat16*>(v_new);
@@ -1397,13 +1408,8 @@ int decode_step(const pp_attn_params* params, const pp_paged_cache* cache, const
   SharedPlan plan = {};
   if (n_groups > 0) {
     plan.units = reinterpret_cast<int64_t*>(ws + L.units);
-    plan.unit_start = reinterpret_cast<int64_t*>(ws + L.unit_start);
-    plan.part_start = reinterpret_cast<int64_t*>(ws + L.part_start);
-    plan.key_tiles = reinterpret_cast<int32_t*>(ws + L.key_tiles);
-    plan.shared_rows = reinterpret_cast<int32_t*>(ws + L.shared_rows);
-    plan.lead = reinterpret_cast<int32_t*>(ws + L.lead);
-    plan.own_start = reinterpret_cast<int32_t*>(ws + L.own_start);
-    plan.group_of = reinterpret_cast<int32_t*>(ws + L.group_of);
+    plan.groups = reinterpret_cast<SharedGroup*>(ws + L.groups);
+    plan.prompts = reinterpret_cast<int2*>(ws + L.prompts);
     plan.q_rot = reinterpret_cast<__nv_bfloat16*>(ws + L.q_rot);
     plan.ml = reinterpret_cast<float2*>(ws + L.shared_ml);
     plan.o = reinterpret_cast<float*>(ws + L.shared_o);
@@ -1416,9 +1422,12 @@ int decode_step(const pp_attn_params* params, const pp_paged_cache* cache, const
     const cudaError_t e = d == 128 ? launch_plan<128>(p, s) : launch_plan<64>(p, s);
     if (e != cudaSuccess) return note_cuda_error((int)e, "plan kernel launch");
     if ((st = launch_shared_attention(*params, a.c, plan, k, a.scale_log2, device_status, s)) != PP_OK) return st;
-    const dim3 rows((unsigned)(((int64_t)k * params->n_q_heads + kCombineThreads / 32 - 1) / (kCombineThreads / 32)));
-    const cudaError_t joined = d == 128 ? launch_dependent(shared_join_kernel<128>, rows, dim3(kCombineThreads), 0, s, a, plan)
-                                        : launch_dependent(shared_join_kernel<64>, rows, dim3(kCombineThreads), 0, s, a, plan);
+    const int64_t heads = (int64_t)k * params->n_q_heads;
+    const bool across = heads <= 8 * kSms;          // as long as a CTA for each runs at once
+    const dim3 blocks((unsigned)(across ? heads : (heads + kCombineThreads / 32 - 1) / (kCombineThreads / 32)));
+    auto join = [&](auto kernel) { return launch_dependent(kernel, blocks, dim3(kCombineThreads), 0, s, a, plan); };
+    const cudaError_t joined = d == 128 ? (across ? join(shared_join_kernel<128, true>) : join(shared_join_kernel<128, false>))
+                                        : (across ? join(shared_join_kernel<64, true>) : join(shared_join_kernel<64, false>));
     if (joined != cudaSuccess) return note_cuda_error((int)joined, "join kernel launch");
   }
   const bool e4m3 = cache->type == PP_CACHE_E4M3;
@@ -1449,13 +1458,8 @@ PagedWorkspace paged_workspace(const pp_attn_params& p, int32_t k, int32_t n_gro
   L.part_o = take(parts * p.head_dim * sizeof(float));
   if (n_groups > 0) {
     L.units = take(sizeof(int64_t));
-    L.unit_start = take(((size_t)n_groups + 1) * sizeof(int64_t));
-    L.part_start = take((size_t)n_groups * sizeof(int64_t));
-    L.key_tiles = take((size_t)n_groups * sizeof(int32_t));
-    L.shared_rows = take((size_t)n_groups * sizeof(int32_t));
-    L.lead = take((size_t)n_groups * sizeof(int32_t));
-    L.own_start = take((size_t)k * sizeof(int32_t));
-    L.group_of = take((size_t)k * sizeof(int32_t));
+    L.groups = take((size_t)n_groups * sizeof(SharedGroup));
+    L.prompts = take((size_t)k * sizeof(int2));
     L.q_rot = take((size_t)k * p.n_q_heads * p.head_dim * sizeof(__nv_bfloat16));
     const size_t rows = (size_t)kSms * kSharedTileRows + 2 * (size_t)k * p.n_q_heads;
     L.shared_ml = take(rows * sizeof(float2));

@@ -58,13 +58,8 @@ struct PagedWorkspace {
   size_t part_ml, part_o;               // float2, float[D]
   // with shared rows only
   size_t units;                         // int64: units in all
-  size_t unit_start;                    // int64 [n_groups + 1]
-  size_t part_start;                    // int64 [n_groups]: part rows before the group's
-  size_t key_tiles;                     // int32 [n_groups]
-  size_t shared_rows;                   // int32 [n_groups]: rows of pages read for the group
-  size_t lead;                          // int32 [n_groups]: the prompt whose row of the page table stands for the group's
-  size_t own_start;                     // int32 [k]: first row that the prompt reads on its own
-  size_t group_of;                      // int32 [k], -1: none
+  size_t groups;                        // SharedGroup [n_groups]
+  size_t prompts;                       // int2 [k]: first row that the prompt reads on its own, its group (-1: none)
   size_t q_rot;                         // bf16 [Hkv][k * group][D]
   size_t shared_ml, shared_o;           // float2, float[D]: parts
   size_t row_ml, row_o;                 // [k][Hq]: joined
@@ -72,11 +67,20 @@ struct PagedWorkspace {
 };
 PagedWorkspace paged_workspace(const pp_attn_params& p, int32_t k, int32_t n_groups);
 
+// A group, as the plan leaves it: what a kernel needs to know of it is one load away.
+struct alignas(16) SharedGroup {
+  int64_t unit_start, part_start;       // units and part rows before the group's
+  int32_t key_tiles;                    // of the shared rows
+  int32_t shared_rows;                  // rows of pages read for the group
+  int32_t lead;                         // the prompt whose row of the page table stands for the group's
+  int32_t first, query_rows;            // first prompt; query rows per KV head
+  int32_t pad[3];
+};
 // The plan of the shared rows as the kernels find it in the workspace.
 struct SharedPlan {
   int64_t* units;
-  int64_t *unit_start, *part_start;
-  int32_t *key_tiles, *shared_rows, *lead, *own_start, *group_of;
+  SharedGroup* groups;
+  int2* prompts;
   __nv_bfloat16* q_rot;
   float2 *ml, *row_ml;
   float *o, *row_o;

@@ -160,30 +160,33 @@ shared_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
           }
           break;
         }
-        int lo = 0, hi = plan.n_groups - 1;       // last group that begins at or before u (those without units come before it)
-        while (lo < hi) {
-          const int mid = (lo + hi + 1) >> 1;
-          if (plan.unit_start[mid] <= u) lo = mid; else hi = mid - 1;
+        // last group that begins at or before u (those without units come before it), 32 candidates at a time
+        int gr = 0;
+        for (int size = plan.n_groups; size > 1;) {
+          const int step = (size + 31) >> 5, at = gr + lane * step;
+          const bool before = lane * step < size && plan.groups[at].unit_start <= u;
+          gr += (__popc(__ballot_sync(0xffffffffu, before)) - 1) * step;
+          size = min(step, plan.n_groups - gr);
         }
-        const int gr = lo, tiles = plan.key_tiles[gr], first = plan.group_ptr[gr];
-        const int rows = (plan.group_ptr[gr + 1] - first) * args.group, row_tiles = (rows + kSharedTileRows - 1) / kSharedTileRows;
-        const int64_t within = u - plan.unit_start[gr];
+        const SharedGroup g = plan.groups[gr];
+        const int tiles = g.key_tiles, rows = g.query_rows, row_tiles = (rows + kSharedTileRows - 1) / kSharedTileRows;
+        const int64_t within = u - g.unit_start;
         const int item = (int)(within / tiles), tile0 = (int)(within - (int64_t)item * tiles);
         const int kv_head = item / row_tiles, rt = item - kv_head * row_tiles;
         const int n = (int)min((int64_t)(tiles - tile0), u_end - u);
-        const int rows_here = min(rows - rt * kSharedTileRows, kSharedTileRows), shared = plan.shared_rows[gr];
-        const int64_t out = (int64_t)blockIdx.x * kSharedTileRows + plan.part_start[gr] + (int64_t)kv_head * shared_part_rows(rows) + rt * kSharedTileRows;
+        const int rows_here = min(rows - rt * kSharedTileRows, kSharedTileRows), shared = g.shared_rows;
+        const int64_t out = (int64_t)blockIdx.x * kSharedTileRows + g.part_start + (int64_t)kv_head * shared_part_rows(rows) + rt * kSharedTileRows;
         if (issue) {
           e[0] = n;
           e[1] = rows_here;
-          e[2] = first * args.group + rt * kSharedTileRows;
+          e[2] = g.first * args.group + rt * kSharedTileRows;
           e[3] = kv_head;
           e[4] = min(shared - (tile0 + n - 1) * BN, BN);       // keys of the piece's last tile
           e[5] = (int)(uint32_t)out;
           e[6] = (int)(out >> 32);
           mbar_arrive(bar_item_full + 8 * ring);
         }
-        const int32_t* table = args.table + (int64_t)plan.lead[gr] * args.table_stride;
+        const int32_t* table = args.table + (int64_t)g.lead * args.table_stride;
         auto page_of = [&](int tile) {            // page of this lane's box; beyond the last one: zeros
           const int key = tile * BN + mine * box_rows;
           if (!lane_issue || tile >= tile0 + n || key >= shared) return args.n_pages;
@@ -392,7 +395,7 @@ shared_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
         tc_fence_after();
         const bool any = first < n;               // (a tile that took no keys leaves l = 0, and its O is not looked at)
         if (row < rows) args.plan.ml[out + row] = make_float2(fmaxf(m_run, -FLT_MAX), sum_f2x2(sum_a, sum_b));
-        float4* dst = reinterpret_cast<float4*>(args.plan.o + (out + row) * D);
+        float* dst = args.plan.o + (out + row) * D;
 #pragma unroll 1
         for (int ch = 0; any && ch < D / 32; ++ch) {
           uint32_t ov[32];
@@ -400,9 +403,10 @@ shared_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
           tc_wait_ld();
           if (row < rows) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-              dst[8 * ch + i] = make_float4(__uint_as_float(ov[4 * i]), __uint_as_float(ov[4 * i + 1]), __uint_as_float(ov[4 * i + 2]),
-                                            __uint_as_float(ov[4 * i + 3]));
+            for (int i = 0; i < 32; i += 8)       // (a lane's own sector: 32 bytes of its row)
+              asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                           ::"l"(dst + 32 * ch + i), "r"(ov[i]), "r"(ov[i + 1]), "r"(ov[i + 2]), "r"(ov[i + 3]), "r"(ov[i + 4]), "r"(ov[i + 5]),
+                             "r"(ov[i + 6]), "r"(ov[i + 7]) : "memory");
           }
         }
         tc_fence_before();
