@@ -30,16 +30,6 @@ __device__ __forceinline__ void angle(int position, double inv_freq, float& cs, 
   red = fma(-n, 2.4492935982947064e-16, red);
   sincosf((float)red, &sn, &cs);
 }
-// Those of four neighbouring elements, one after another: the code of a sine is long, and instructions have to be fetched too.
-__device__ __forceinline__ void angles4(int position, const double* inv_freq, float (&cs)[4], float (&sn)[4]) {
-#pragma unroll 1
-  for (int e = 0; e < 4; ++e) {
-    float c, s;
-    angle(position, inv_freq[e], c, s);
-    cs[0] = cs[1]; cs[1] = cs[2]; cs[2] = cs[3]; cs[3] = c;
-    sn[0] = sn[1]; sn[1] = sn[2]; sn[2] = sn[3]; sn[3] = s;
-  }
-}
 __device__ __forceinline__ float turn_lo(float a, float b, float cs, float sn) { return __fmaf_rn(a, cs, -__fmul_rn(b, sn)); }
 __device__ __forceinline__ float turn_hi(float a, float b, float cs, float sn) { return __fmaf_rn(b, cs, __fmul_rn(a, sn)); }
 
@@ -196,21 +186,29 @@ append_kernel(const __grid_constant__ AppendArgs a) {
 // ------------------------------------------------------------------------------------------
 // One generation step
 // ------------------------------------------------------------------------------------------
+// Two kernels, and a third for what the second one cuts:
+//   step_prepare_kernel   a CTA for each prompt: rotates its queries, rotates and appends the new token. (With shared rows a further
+//                         CTA lays their work out, see below.)
+//   paged_decode_kernel   attention over the rows, the appended one like any other
+//   paged_combine_kernel  joins the parts of items that were cut
 // Bound: HBM, every row of K and V is read once. The work is a line of units of 8 KB (16, 32 or 64 rows of K and V of one KV
 // head), ordered by (prompt, KV head, rows), and cut into equal pieces, one for each warp that the GPU holds: all warps read the
 // same number of bytes whatever the lengths are. A warp works on its own from there on. Its rows arrive by TMA in a ring of
 // two units in shared memory, whose loads run ahead over the ends of items. Six warps (seven over 8-bit pages, which take more
 // instructions a byte) keep up to 96 KB of an SM under way, which is all that HBM takes: with twelve, the loads queued up and SMs
-// were served so unevenly that of 148 equal shares the last ended 20 % after the mean. A piece that is a whole item (prompt, KV head) leaves O at once; of an item that is cut the parts (m, l, o) are joined by
-// paged_combine_kernel.
+// were served so unevenly that of 148 equal shares the last ended 20 % after the mean. A piece that is a whole item (prompt, KV head)
+// leaves O at once. What an item costs beside its rows is the latency of one warp: with the queries rotated there, and the new token a step
+// of its own, 4700 cycles of 1800 a unit (64 prompts on 32 heads 57.8 -> PREP7B us, 256 prompts behind 8192 shared rows 114 -> PREPSYS).
 // The arithmetic is that of the step over contiguous caches (pp_decode.cu): mma.m16n8k16 with 16 keys as rows and the query heads
 // of a KV head as the 8 columns, absent heads 0. Over bf16 pages a query and a weight each reach it as the sum of two
 // 16-bit numbers: HBM leaves the tensor cores idle, and scores and O are then exact to 2^-16, far below O's last rounding of 2^-8.
 // The lengths live on the device: every CTA sums them itself, and the grid and the room for parts depend on neither them nor k.
+// (It does so before its wait for the kernel in front, which, like all kernels here, lets the next one start only after its own wait:
+// what that one waited for is there then. Not through L1, which may hold what it was before.)
 constexpr int kMaxGroup = 8;            // query heads per KV head: the N of the tensor-core product
 constexpr int kMostStepWarps = 7, kMostPieces = kSms * kMostStepWarps;
 constexpr int kHalfUnit = 4096;         // bytes of K, and of V, in a unit
-constexpr int kScratch = 2304;          // per warp: queries, the new token's rows, O on its way out
+constexpr int kScratch = 2048;          // per warp: O on its way out
 constexpr int kCombineThreads = 256;
 // The running maximum of a row moves only when a score exceeds it by more than 2^kLazyLog2: until then no lane has to ask the
 // others (three exchanges for each of two heads). Sums are at most 2^kLazyLog2 as large, which costs fp32 nothing.
@@ -225,6 +223,8 @@ struct PagedArgs {
   int64_t q_stride, k_stride, v_stride;
   __nv_bfloat16* o;
   int4* cut;                            // [pieces]: of the item that begins in a piece and ends in another: prompt, KV head, pieces; 0 pieces: none
+  uint32_t* q;                          // queries as the products take them: [prompt][head][t][parts][D / 8] words, see Rows
+  float* q_factor;                      // [prompt][head] over 8-bit pages: from a product with them to scaled log2 units
   float2* part_ml;                      // [2 pieces][group]
   float* part_o;                        // [2 pieces][group][D]
   int32_t n_prompts, n_q_heads, n_kv_heads, group;
@@ -236,7 +236,7 @@ struct PagedArgs {
 
 // Rows that the pages hold for prompt i before the step; -1 for a row of no prompt, and for a length that its table row has no room for.
 __device__ __forceinline__ int checked_length(const PagedCacheArgs& c, const int32_t* lengths, int i, bool fresh, int32_t* status) {
-  const int len = lengths[i];
+  const int len = __ldcg(lengths + i);
   const int64_t room = (int64_t)c.table_stride << c.page_shift;
   if (len + (int64_t)fresh > room) {
     note_status(status, PP_PAGED_BAD_LENGTH);
@@ -321,18 +321,14 @@ struct Rows<D, false> {
   static constexpr int kWarps = 6;
   static constexpr int kRowBytes = 2 * D, kSteps = kHalfUnit / (16 * kRowBytes);      // steps of 16 keys in a unit
   static constexpr float kWeight = 1.f;
-  static constexpr bool kLowPart = true;
+  static constexpr int kParts = 2;                    // 16-bit parts of a query
+  // which thread t takes the pair of elements (e, e + 1) of a query, and as which of its D / 8 words
+  static __device__ __forceinline__ int word_thread(int e) { return (e >> 1) & 3; }
+  static __device__ __forceinline__ int word_index(int e) { return (e >> 4) * 2 + ((e >> 3) & 1); }
   // A step's box, as TMA leaves it: chunks of 64 elements one behind the other, rows of 128 bytes, the 16-byte pieces of 8 rows
   // swizzled so that one of each row fill all banks once.
   static constexpr int kStepBytes = 16 * kRowBytes, kChunkBytes = 2048;
   static __device__ __forceinline__ int row_of(int at) { return (D == 128 ? 0 : (at >> 11) * 16) + ((at >> 7) & 15); }   // of byte `at` of a unit
-  static __device__ __forceinline__ void load_q(uint32_t (&q)[D / 8], uint32_t row_at, int t) {
-#pragma unroll
-    for (int kk = 0; kk < D / 16; ++kk)
-#pragma unroll
-      for (int x = 0; x < 2; ++x)
-        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(q[2 * kk + x]) : "r"(row_at + 32 * kk + 16 * x + 4 * t) : "memory");
-  }
   static __device__ __forceinline__ void mma_scores(float (&c)[4], const uint32_t (*a)[4], const uint32_t (&qh)[D / 8], const uint32_t (&ql)[D / 8]) {
     // four chains of products instead of one: each waits for the one before it
     float p[4][4];
@@ -352,21 +348,6 @@ struct Rows<D, false> {
     const uint32_t from = at + ((lane & 7) + (lane & 8)) * 128 + (((lane >> 4) ^ (lane & 7)) << 4);
 #pragma unroll
     for (int kk = 0; kk < D / 16; ++kk) ldmatrix4(a[kk], (from ^ ((kk & 3) << 5)) + (kk >> 2) * kChunkBytes);
-    mma_scores(c, a, qh, ql);
-  }
-  // a row of its own, as the first of 16
-  static __device__ __forceinline__ void scores_one(float (&c)[4], uint32_t at, const uint32_t (&qh)[D / 8], const uint32_t (&ql)[D / 8], int g, int t) {
-    uint32_t a[D / 16][4];
-#pragma unroll
-    for (int kk = 0; kk < D / 16; ++kk) {
-      uint32_t x, y;
-      asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x) : "r"(at + 32 * kk + 4 * t) : "memory");
-      asm volatile("ld.shared.u32 %0, [%1];" : "=r"(y) : "r"(at + 32 * kk + 16 + 4 * t) : "memory");
-      a[kk][0] = g == 0 ? x : 0u;
-      a[kk][1] = 0u;
-      a[kk][2] = g == 0 ? y : 0u;
-      a[kk][3] = 0u;
-    }
     mma_scores(c, a, qh, ql);
   }
   // P in two parts of 8 bits, the first cut and not rounded, so that neither is negative, and none of a weight above 0 (which is
@@ -398,16 +379,6 @@ struct Rows<D, false> {
       uint32_t a[4];
       ldmatrix4_trans(a, (from ^ ((j & 3) << 5)) + (j >> 2) * kChunkBytes);
       add(acc[j], a[0], a[1], a[2], a[3], w);
-    }
-  }
-  static __device__ __forceinline__ void product_one(float (&acc)[D / 16][4], uint32_t at, const float (&p)[4], int g, int t) {
-    const Weights w = weights(p);
-#pragma unroll
-    for (int j = 0; j < D / 16; ++j) {
-      uint16_t x, y;
-      asm volatile("ld.shared.u16 %0, [%1];" : "=h"(x) : "r"(at + 2 * (16 * j + g)) : "memory");
-      asm volatile("ld.shared.u16 %0, [%1];" : "=h"(y) : "r"(at + 2 * (16 * j + g + 8)) : "memory");
-      add(acc[j], t == 0 ? x : 0u, t == 0 ? y : 0u, 0u, 0u, w);
     }
   }
   // element of O that acc[j][0], acc[j][1] (x = 0) and acc[j][2], acc[j][3] (x = 1) stand for
@@ -446,19 +417,14 @@ struct Rows<D, true> {
   // Queries and weights are rounded to f16 once: 11 bits, 2^-12 of each, against the 2^-8 of O's last rounding and keys of 4 bits.
   // Weights are at most 2^kLazyLog2; times 2^11 those down to 2^-25 of the largest have all of their bits, and what the sum of 2^17
   // of the smallest loses is below 2^-18 of it.
-  static constexpr bool kLowPart = false;
+  static constexpr int kParts = 1;
+  static __device__ __forceinline__ int word_thread(int e) { return e / (D / 4); }
+  static __device__ __forceinline__ int word_index(int e) { return e % (D / 4) / 2; }
   static constexpr float kWeight = 2048.f;
   // A step's box, as TMA leaves it: rows of 128 (64) bytes, whose 16-byte pieces are swizzled.
   static constexpr int kStepBytes = 16 * kRowBytes;
   static __device__ __forceinline__ uint32_t place(int row, int piece) { return row * D + ((piece ^ (D == 128 ? row & 7 : (row >> 1) & 3)) << 4); }
   static __device__ __forceinline__ int row_of(int at) { return at / D; }
-  static __device__ __forceinline__ void load_q(uint32_t (&q)[D / 8], uint32_t row_at, int t) {
-#pragma unroll
-    for (int i = 0; i < D / 32; ++i) {                // words 8 (piece) + 2 (word of the piece) + pair
-      const uint4 x = shared16(row_at + D / 2 * t + 16 * i);
-      q[4 * i] = x.x; q[4 * i + 1] = x.y; q[4 * i + 2] = x.z; q[4 * i + 3] = x.w;
-    }
-  }
   static __device__ __forceinline__ void mma_scores(float (&c)[4], const uint4 (&r0)[D / 64], const uint4 (&r1)[D / 64], const uint32_t (&q)[D / 8]) {
     float p[2][4];
 #pragma unroll
@@ -481,17 +447,6 @@ struct Rows<D, true> {
     for (int i = 0; i < D / 64; ++i) {
       r0[i] = shared16(at + place(g, D / 64 * t + i));
       r1[i] = shared16(at + place(g + 8, D / 64 * t + i));
-    }
-    mma_scores(c, r0, r1, q);
-  }
-  static __device__ __forceinline__ void scores_one(float (&c)[4], uint32_t at, const uint32_t (&q)[D / 8], const uint32_t (&)[D / 8], int g, int t) {
-    uint4 r0[D / 64], r1[D / 64];
-    const uint4 none = make_uint4(0u, 0u, 0u, 0u);
-#pragma unroll
-    for (int i = 0; i < D / 64; ++i) {
-      const uint4 x = shared16(at + 16 * (D / 64 * t + i));
-      r0[i] = g == 0 ? x : none;
-      r1[i] = none;
     }
     mma_scores(c, r0, r1, q);
   }
@@ -531,15 +486,6 @@ struct Rows<D, true> {
 #pragma unroll
     for (int n = 0; n < D / 32; ++n) add(acc, n, word_of(r[0], n), word_of(r[1], n), word_of(r[2], n), word_of(r[3], n), w);
   }
-  static __device__ __forceinline__ void product_one(float (&acc)[D / 16][4], uint32_t at, const float (&p)[4], int g, int t) {
-    const Weights w = weights(p);
-#pragma unroll
-    for (int n = 0; n < D / 32; ++n) {
-      uint32_t x;
-      asm volatile("ld.shared.u32 %0, [%1];" : "=r"(x) : "r"(at + (D / 8) * g + 4 * n) : "memory");
-      add(acc, n, t == 0 ? x : 0u, 0u, 0u, 0u, w);
-    }
-  }
   static __device__ __forceinline__ int element(int j, int x, int g) { return (D / 8) * g + 2 * j + x; }
   static __device__ __forceinline__ int element_at(int place) { return place; }
   static __device__ __forceinline__ void leave(const float (&acc)[D / 16][4], float f0, float f1, uint32_t at, int g, int t) {
@@ -559,14 +505,12 @@ struct Rows<D, true> {
 };
 
 // A warp's place on the line: the part of an item (prompt i, KV head kvh) that lies in its piece. An item takes kItemUnits of the line
-// more than it has units: what its beginning and end cost its warp. With 1, 2, 3, 4 and 6 (seven warps; us a step): 256 prompts behind
-// 8192 shared rows -, 128, 124, 122, 122; 256 prompts of two lengths, 240 k rows, 32 / 8 heads -, 166, 168, 169, 168, in e4m3 -, 101, 92,
-// 94, 98; 64 prompts on 32 heads -, 55.8, 56.6, 57.8, 59.0.
-constexpr int kItemUnits = 3;
+// more than it has units: what its beginning and end cost its warp.
+constexpr int kItemUnits = 2;
 struct Place {
   int64_t left;                         // of the piece, from here on
   int i, kvh;
-  int len, start;                       // rows of the prompt, first row that is read here
+  int len, start;                       // rows of the prompt, the new one among them; first row that is read here
   int units;                            // of an item of this prompt
   int off, n;                           // units off .. off + n - 1 of the item
   int used;                             // of the piece by this part
@@ -583,7 +527,8 @@ struct Line {
     start = 0;
     if (i < a.n_prompts) {
       len = checked_length(a.c, a.lengths, i, fresh, nullptr);
-      if (a.own) start = a.own[i].x;
+      if (len >= 0) len += fresh;
+      if (a.own) start = __ldcg(&a.own[i].x);
     }
   }
   __device__ __forceinline__ int64_t line_units(int len, int start) const { return (int64_t)(units(len, start) + kItemUnits) * a.n_kv_heads; }
@@ -624,10 +569,8 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                     const __grid_constant__ SharedPlan plan) {
   using R = Rows<D, kE4m3>;
   constexpr int kWarps = R::kWarps, kThreads = 32 * kWarps, kPieces = kSms * kWarps;
-  constexpr int kSteps = R::kSteps, kUnitRows = 16 * kSteps, kHalf = D / 2, kSize = kE4m3 ? 1 : 2;
-  constexpr int kLanesPerHead = kHalf / 4, kHeadsAtOnce = 32 / kLanesPerHead;       // queries: four (j, j + D/2) pairs a lane
-  constexpr int kQPitch = 2 * D + 16;                                               // bytes
-  static_assert(kMaxGroup * kQPitch <= kScratch && kMaxGroup * D * 2 <= kScratch && 4 * D <= kScratch, "scratch");
+  constexpr int kSteps = R::kSteps, kUnitRows = 16 * kSteps, kWords = R::kParts * D / 8;
+  static_assert(kMaxGroup * D * 2 <= kScratch, "scratch");
   extern __shared__ __align__(1024) uint8_t s_dyn[];
   __shared__ int64_t s_warp[kWarps], s_before[kThreads];
   __shared__ uint64_t s_bar[kWarps][4];                 // K of two units, V of two units
@@ -643,15 +586,12 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   const WaitCtx wctx{smem_u32(&s_abort), a.wait_limit, a.status};
-  pdl_wait();                           // lengths, table, pages: all may come from the kernel before
-  pdl_launch_dependents();
-
   // ---- the line, and this warp's piece of it
   const int each = (a.n_prompts + kThreads - 1) / kThreads;
   int64_t mine = 0, total;
   for (int i = tid * each; i < min((tid + 1) * each, a.n_prompts); ++i) {
     const int len = checked_length(a.c, a.lengths, i, fresh, blockIdx.x == 0 ? a.status : nullptr);
-    if (len >= 0) mine += line.line_units(len, a.own ? a.own[i].x : 0);
+    if (len >= 0) mine += line.line_units(len + fresh, a.own ? __ldcg(&a.own[i].x) : 0);
   }
   s_before[tid] = block_prefix<kThreads>(mine, s_warp, total);
   __syncthreads();
@@ -661,7 +601,7 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
   Place c;                              // where the arithmetic is
   c.left = min(per, total - u0);
   if (lane == 0) a.cut[piece] = make_int4(0, 0, 0, 0);
-  if (c.left <= 0) return;
+  if (c.left <= 0) return pdl_wait();   // (the kernel after this one counts on all in front of it)
   {
     int lo = 0;                         // last thread whose prompts begin at or before u0 (those without units come before it)
     for (int w = 0; w < kWarps; ++w) lo += __popc(__ballot_sync(0xffffffffu, s_before[32 * w + lane] <= u0));
@@ -676,7 +616,7 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
     }
     line.enter(c, at);
     if (c.n == 0) line.advance(c);      // a piece that ends before the item's first unit leaves it to the next
-    if (c.n == 0) return;
+    if (c.n == 0) return pdl_wait();
   }
 
   // ---- loads, which run ahead
@@ -695,7 +635,7 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
     const int64_t row = f.start + ((int64_t)batch * 32 + lane) * 16;
     ids = 0;
     if (row < f.len) {
-      ids = a.c.table[(int64_t)f.i * a.c.table_stride + (row >> a.c.page_shift)];
+      ids = __ldcg(a.c.table + (int64_t)f.i * a.c.table_stride + (row >> a.c.page_shift));
       if ((unsigned)ids >= (unsigned)a.c.n_pages) {
         note_status(a.status, PP_PAGED_BAD_PAGE);
         ids = 0;
@@ -724,50 +664,53 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
       f_at = 0;
     }
   };
-  load_k();
-  load_v();
-  load_k();
-  load_v();
+  // Rows that were there before the step need not wait for it to be prepared.
+  int loaded = 0;
+  for (; loaded < 2 && f.n > 0 && f.start + (f.off + f_at + 1) * kUnitRows <= f.len - (int)fresh; ++loaded) {
+    load_k();
+    load_v();
+  }
+  pdl_wait();                           // the queries and the appended rows
+  pdl_launch_dependents();
+  for (; loaded < 2; ++loaded) {
+    load_k();
+    load_v();
+  }
 
   uint32_t stage = 0, phase = 0;
-  int angles_of = -1;
-  float cs[4], sn[4];                   // of this lane's four pairs, at the position of prompt angles_of
-  const int j0 = 4 * (lane % kLanesPerHead);
   // A wait gave up: loads of this warp may still be in flight. They get time to land before shared memory is handed back.
   auto settle = [&]() {
     const unsigned long long t0 = global_ns();
     while (global_ns() - t0 < 100000ull) {}
   };
-  // What a part of an item needs beside its rows: four (j, j + D/2) pairs of the lane's heads, and of the new token.
-  struct Raw { uint2 lo[kMaxGroup / kHeadsAtOnce], hi[kMaxGroup / kHeadsAtOnce], new_lo, new_hi, new_v; };
-  auto ends_item = [&](const Place& p) { return p.off + p.n == p.units; };
-  auto fetch = [&](Raw& r, const Place& p) {
-    const __nv_bfloat16* q_row = a.q_new + (int64_t)p.i * a.q_stride + (int64_t)p.kvh * a.group * D;
+  // The queries of an item, of head g (zeros for absent heads), and of heads 2t and 2t + 1 the factor of their scores.
+  struct Queries { uint32_t w[kWords]; float factor[2]; };
+  auto fetch = [&](Queries& q, const Place& p) {
+    const int64_t head = (int64_t)p.i * a.n_q_heads + p.kvh * a.group;
+    const uint4* from = reinterpret_cast<const uint4*>(a.q + (head + g) * (4 * kWords) + t * kWords);
 #pragma unroll
-    for (int x = 0; x < kMaxGroup / kHeadsAtOnce; ++x) {
-      const int h = x * kHeadsAtOnce + lane / kLanesPerHead;
-      r.lo[x] = r.hi[x] = make_uint2(0u, 0u);
-      if (h < a.group) {
-        r.lo[x] = *reinterpret_cast<const uint2*>(q_row + h * D + j0);
-        r.hi[x] = *reinterpret_cast<const uint2*>(q_row + h * D + j0 + kHalf);
-      }
+    for (int x = 0; x < kWords / 4; ++x) {
+      const uint4 w = g < a.group ? __ldcg(from + x) : make_uint4(0u, 0u, 0u, 0u);
+      q.w[4 * x] = w.x; q.w[4 * x + 1] = w.y; q.w[4 * x + 2] = w.z; q.w[4 * x + 3] = w.w;
     }
-    if (fresh && ends_item(p)) {
-      const __nv_bfloat16* k_row = a.k_new + (int64_t)p.i * a.k_stride + p.kvh * D;
-      r.new_lo = *reinterpret_cast<const uint2*>(k_row + j0);
-      r.new_hi = *reinterpret_cast<const uint2*>(k_row + j0 + kHalf);
-      r.new_v = *reinterpret_cast<const uint2*>(a.v_new + (int64_t)p.i * a.v_stride + p.kvh * D + 4 * (lane % (D / 4)));
-    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) q.factor[h] = kE4m3 && 2 * t + h < a.group ? __ldcg(a.q_factor + head + 2 * t + h) : a.scale_log2;
   };
-  Raw raw, raw_next;
-  fetch(raw_next, c);
+  Queries next_q;
+  fetch(next_q, c);
   while (true) {
     // ---- a part of an item; the queries of the next one are on their way meanwhile
-    const bool begins = c.off == 0, ends = ends_item(c), new_row = ends && fresh;
-    raw = raw_next;
+    const bool begins = c.off == 0, ends = c.off + c.n == c.units;
+    uint32_t qh[D / 8], ql[D / 8];
+#pragma unroll
+    for (int x = 0; x < D / 8; ++x) {
+      qh[x] = next_q.w[x];
+      ql[x] = R::kParts == 2 ? next_q.w[(R::kParts - 1) * (D / 8) + x] : 0u;
+    }
+    const float scale[2] = {next_q.factor[0], next_q.factor[1]};
     Place next = c;
     line.advance(next);
-    if (next.n > 0) fetch(raw_next, next);
+    if (next.n > 0) fetch(next_q, next);
     // (m, l) and o over the rows that the prompt shares, where this part is the item's first
     float m[2] = {kNoScore, kNoScore}, l[2] = {0.f, 0.f}, acc[D / 16][4];
 #pragma unroll
@@ -778,83 +721,17 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
         const int head = 2 * t + h;
         if (head >= a.group) continue;
         const int64_t at = (int64_t)c.i * a.n_q_heads + c.kvh * a.group + head;
-        const float2 ml = plan.row_ml[at];
+        const float2 ml = __ldcg(plan.row_ml + at);
         m[h] = ml.x;
         l[h] = g == 0 ? ml.y : 0.f;
         const float4* from = reinterpret_cast<const float4*>(plan.row_o + at * D + (D / 8) * g);
 #pragma unroll
         for (int j = 0; j < D / 16; j += 2) {
-          const float4 x = from[j >> 1];
+          const float4 x = __ldcg(from + (j >> 1));
           acc[j][h] = x.x; acc[j][2 + h] = x.y;
           acc[j + 1][h] = x.z; acc[j + 1][2 + h] = x.w;
         }
       }
-    }
-    if (angles_of != c.i) {
-      angles_of = c.i;
-      angles4(fresh ? c.len : max(c.len - 1, 0), a.angles.inv_freq + j0, cs, sn);
-    }
-    auto turn = [&](uint2 lo, uint2 hi, float (&p)[4], float (&y)[4]) {
-      const float2 p0 = unpack_bf16(lo.x), p1 = unpack_bf16(lo.y), y0 = unpack_bf16(hi.x), y1 = unpack_bf16(hi.y);
-      const float x[4] = {p0.x, p0.y, p1.x, p1.y}, z[4] = {y0.x, y0.y, y1.x, y1.y};
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        p[e] = turn_lo(x[e], z[e], cs[e], sn[e]);
-        y[e] = turn_hi(x[e], z[e], cs[e], sn[e]);
-      }
-    };
-    const float k_scale = kE4m3 ? a.c.k_scale[c.kvh] : 1.f, v_scale = kE4m3 ? a.c.v_scale[c.kvh] : 1.f;
-    uint32_t qh[D / 8], ql[D / 8];
-    float scale[2] = {a.scale_log2, a.scale_log2};
-    // the upper parts through the scratch memory, then the lower ones, which wait in `raw`
-#pragma unroll
-    for (int x = 0; x < kMaxGroup / kHeadsAtOnce; ++x) {
-      if (x * kHeadsAtOnce >= a.group) break;
-      const int h = x * kHeadsAtOnce + lane / kLanesPerHead;
-      float p[4], y[4];
-      turn(raw.lo[x], raw.hi[x], p, y);
-      if constexpr (kE4m3) {
-        // f16 has 5 exponent bits: a query is brought to below 2 by a power of two (of up to 2^120: the rest f16 has room
-        // for), which goes into its factor
-        float top = 0.f;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) top = fmaxf(top, fmaxf(fabsf(p[e]), fabsf(y[e])));
-#pragma unroll
-        for (int o = kLanesPerHead / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-        const int shift = min(max((int)(__float_as_uint(top) >> 23) - 127, -120), 120);
-        const float down = __uint_as_float((uint32_t)(127 - shift) << 23), factor = a.scale_log2 * k_scale * __uint_as_float((uint32_t)(127 + shift) << 23);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) { p[e] *= down; y[e] *= down; }
-#pragma unroll
-        for (int z = 0; z < 2; ++z) {       // heads 2t and 2t + 1 are this lane's columns
-          const float other = __shfl_sync(0xffffffffu, factor, ((2 * t + z) % kHeadsAtOnce) * kLanesPerHead);
-          if ((2 * t + z) / kHeadsAtOnce == x) scale[z] = other;
-        }
-      }
-      const uint32_t w[4] = {R::high(p[0], p[1]), R::high(p[2], p[3]), R::high(y[0], y[1]), R::high(y[2], y[3])};
-      *reinterpret_cast<uint2*>(scratch_p + h * kQPitch + 2 * j0) = make_uint2(w[0], w[1]);
-      *reinterpret_cast<uint2*>(scratch_p + h * kQPitch + 2 * (j0 + kHalf)) = make_uint2(w[2], w[3]);
-      raw.lo[x] = make_uint2(R::low(p[0], p[1], w[0]), R::low(p[2], p[3], w[1]));
-      raw.hi[x] = make_uint2(R::low(y[0], y[1], w[2]), R::low(y[2], y[3], w[3]));
-    }
-    __syncwarp();
-    R::load_q(qh, scratch + g * kQPitch, t);
-    __syncwarp();
-    if constexpr (R::kLowPart) {
-#pragma unroll
-      for (int x = 0; x < kMaxGroup / kHeadsAtOnce; ++x) {
-        if (x * kHeadsAtOnce >= a.group) break;
-        const int h = x * kHeadsAtOnce + lane / kLanesPerHead;
-        *reinterpret_cast<uint2*>(scratch_p + h * kQPitch + 2 * j0) = raw.lo[x];
-        *reinterpret_cast<uint2*>(scratch_p + h * kQPitch + 2 * (j0 + kHalf)) = raw.hi[x];
-      }
-      __syncwarp();
-      R::load_q(ql, scratch + g * kQPitch, t);
-      __syncwarp();
-    }
-    if (g >= a.group) {                 // absent heads
-#pragma unroll
-      for (int x = 0; x < D / 8; ++x) qh[x] = ql[x] = 0u;
     }
 
     // ---- the rows
@@ -921,55 +798,15 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
       stage ^= 1;
       phase ^= stage ^ 1;               // (after every second unit)
     }
-    if (new_row) {                      // the new token, and its rows of the pages
-      float p[4], y[4];
-      turn(raw.new_lo, raw.new_hi, p, y);
-      const float2 v0 = unpack_bf16(raw.new_v.x), v1 = unpack_bf16(raw.new_v.y);
-      if constexpr (kE4m3) {
-        const float per_k = __frcp_rn(k_scale), per_v = __frcp_rn(v_scale);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) { p[e] *= per_k; y[e] *= per_k; }
-        if (lane < kLanesPerHead) {
-          *reinterpret_cast<uint32_t*>(scratch_p + j0) = round_e4m3(p[0], p[1], p[2], p[3]);
-          *reinterpret_cast<uint32_t*>(scratch_p + j0 + kHalf) = round_e4m3(y[0], y[1], y[2], y[3]);
-        }
-        if (lane < D / 4)
-          *reinterpret_cast<uint32_t*>(scratch_p + D + 4 * lane) =
-              round_e4m3(v0.x * per_v, v0.y * per_v, v1.x * per_v, v1.y * per_v);
-      } else {
-        if (lane < kLanesPerHead) {
-          *reinterpret_cast<uint2*>(scratch_p + 2 * j0) = make_uint2(round_bf16(p[0], p[1]), round_bf16(p[2], p[3]));
-          *reinterpret_cast<uint2*>(scratch_p + 2 * (j0 + kHalf)) = make_uint2(round_bf16(y[0], y[1]), round_bf16(y[2], y[3]));
-        }
-        if (lane < D / 4) *reinterpret_cast<uint2*>(scratch_p + 2 * D + 8 * lane) = raw.new_v;
-      }
-      __syncwarp();
-      float s[1][4];
-      R::scores_one(s[0], scratch, qh, ql, g, t);
-      soften(s, 1);
-      R::product_one(acc, scratch + D * kSize, s[0], g, t);
-      const int page = a.c.table[(int64_t)c.i * a.c.table_stride + (c.len >> a.c.page_shift)];
-      if ((unsigned)page < (unsigned)a.c.n_pages) {
-        const int64_t to = (int64_t)page * a.c.page_stride + (int64_t)c.kvh * a.c.head_stride + (int64_t)(c.len & row_mask) * a.c.row_stride;
-        if (lane < R::kRowBytes / 16) {
-          *reinterpret_cast<uint4*>(a.c.k_pages + to + 16 * lane) = shared16(scratch + 16 * lane);
-          *reinterpret_cast<uint4*>(a.c.v_pages + to + 16 * lane) = shared16(scratch + D * kSize + 16 * lane);
-        }
-      } else if (lane == 0) {
-        note_status(a.status, PP_PAGED_BAD_PAGE);
-      }
-      __syncwarp();
-    }
-
     // ---- out
-    const float out_scale = v_scale / R::kWeight;
+    const float out_scale = (kE4m3 ? a.c.v_scale[c.kvh] : 1.f) / R::kWeight;
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int o = 4; o < 32; o <<= 1) l[h] += __shfl_xor_sync(0xffffffffu, l[h], o);
     if (begins && ends) {
       // (a row that attends to nothing is 0; one all of whose scores are -inf is a NaN)
-      const bool none = c.len + (int)fresh <= 0;
+      const bool none = c.len == 0;
       R::leave(acc, none ? 0.f : out_scale / l[0], none ? 0.f : out_scale / l[1], scratch, g, t);
       __syncwarp();
       __nv_bfloat16* to = a.o + ((int64_t)c.i * a.n_q_heads + c.kvh * a.group) * D;
@@ -1018,13 +855,13 @@ __device__ __forceinline__ Joined<D> join_parts(int first, int step, int n, cons
       for (int e = 0; e < E; ++e) p[c][e] = 0.f;
       if (base + c * step >= n) continue;
       const int64_t from = at(base + c * step);
-      ml[c] = mls[from];
+      ml[c] = __ldcg(mls + from);
       const float* src = os + from * D + E * lane;
       if constexpr (E == 4) {
-        const float4 x = *reinterpret_cast<const float4*>(src);
+        const float4 x = __ldcg(reinterpret_cast<const float4*>(src));
         p[c][0] = x.x; p[c][1] = x.y; p[c][2] = x.z; p[c][3] = x.w;
       } else {
-        const float2 x = *reinterpret_cast<const float2*>(src);
+        const float2 x = __ldcg(reinterpret_cast<const float2*>(src));
         p[c][0] = x.x; p[c][1] = x.y;
       }
     }
@@ -1116,20 +953,22 @@ paged_combine_kernel(const __grid_constant__ PagedArgs a, int n_pieces) {
 }
 
 // ------------------------------------------------------------------------------------------
-// Plan of a step with shared rows
+// What a step prepares
 // ------------------------------------------------------------------------------------------
-// CTA i < k rotates the queries of prompt i into the rows that the tensor cores read. The last CTA lays the work out: how many
-// rows each group really shares (no more than its shortest prompt has, whole pages), and the line of units.
-constexpr int kPlanThreads = 512;
-struct PlanArgs {
+// CTAs (i < k, part): prompt i's queries, rotated, in the order of the words that the products take (and, with shared rows, as rows for the
+// tensor cores of their kernel); its new token's key, rotated, and value, into its pages. With shared rows the last CTA lays their
+// work out: how many rows each group really shares (no more than its shortest prompt has, whole pages), and the line of units.
+constexpr int kPrepareThreads = 256;
+struct PrepareArgs {
   PagedArgs a;
   SharedPlan plan;
   const int32_t* shared_len;
 };
 
-template <int D>
-__global__ void __launch_bounds__(kPlanThreads)
-shared_plan_kernel(const __grid_constant__ PlanArgs p) {
+template <int D, bool kE4m3>
+__global__ void __launch_bounds__(kPrepareThreads)
+step_prepare_kernel(const __grid_constant__ PrepareArgs p) {
+  using R = Rows<D, kE4m3>;
   const PagedArgs& a = p.a;
   const SharedPlan& plan = p.plan;
   const int tid = threadIdx.x, k = a.n_prompts;
@@ -1137,38 +976,103 @@ shared_plan_kernel(const __grid_constant__ PlanArgs p) {
   pdl_wait();
   pdl_launch_dependents();
   if ((int)blockIdx.x < k) {
-    constexpr int kHalf = D / 2, kUnits = kHalf / 4;
-    __shared__ float s_cos[kHalf], s_sin[kHalf];
-    const int i = blockIdx.x, len = a.lengths[i];
-    if (len < 0) return;                // (its rows of the tiles hold what they held: nothing of them is read)
-    if (tid < kHalf) angle(fresh ? len : max(len - 1, 0), a.angles.inv_freq[tid], s_cos[tid], s_sin[tid]);
-    __syncthreads();
-    for (int u = tid; u < a.n_q_heads * kUnits; u += kPlanThreads) {
-      const int h = u / kUnits, j = 4 * (u - h * kUnits), kvh = h / a.group;
-      const __nv_bfloat16* src = a.q_new + (int64_t)i * a.q_stride + (int64_t)h * D + j;
-      __nv_bfloat16* dst = plan.q_rot + (((int64_t)kvh * k + i) * a.group + h - kvh * a.group) * D + j;
-      const uint2 lo = *reinterpret_cast<const uint2*>(src), hi = *reinterpret_cast<const uint2*>(src + kHalf);
-      const float2 p0 = unpack_bf16(lo.x), p1 = unpack_bf16(lo.y), y0 = unpack_bf16(hi.x), y1 = unpack_bf16(hi.y);
-      const float x[4] = {p0.x, p0.y, p1.x, p1.y}, y[4] = {y0.x, y0.y, y1.x, y1.y};
-      float rx[4], ry[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        rx[e] = turn_lo(x[e], y[e], s_cos[j + e], s_sin[j + e]);
-        ry[e] = turn_hi(x[e], y[e], s_cos[j + e], s_sin[j + e]);
+    constexpr int kHalf = D / 2, kUnits = kHalf / 4, kSize = kE4m3 ? 1 : 2;      // units: four (j, j + D/2) pairs of a head
+    __shared__ __align__(16) float s_cos[kHalf], s_sin[kHalf];
+    const int i = blockIdx.x, len = checked_length(a.c, a.lengths, i, fresh, nullptr);
+    if (len < 0) return;                // (what its rows of the workspace hold is not read)
+    int64_t to = -1;                    // byte offset of the new row
+    if (fresh) {
+      const int page = a.c.table[(int64_t)i * a.c.table_stride + (len >> a.c.page_shift)];
+      if ((unsigned)page < (unsigned)a.c.n_pages) to = (int64_t)page * a.c.page_stride + (int64_t)(len & ((1 << a.c.page_shift) - 1)) * a.c.row_stride;
+      else if (tid == 0) note_status(a.status, PP_PAGED_BAD_PAGE);
+    }
+    const __nv_bfloat16 *q = a.q_new + (int64_t)i * a.q_stride, *kn = a.k_new + (int64_t)i * a.k_stride, *vn = a.v_new + (int64_t)i * a.v_stride;
+    const int q_units = a.n_q_heads * kUnits, units = q_units + (to >= 0 ? a.n_kv_heads * kUnits : 0);
+    for (int u0 = blockIdx.y * kPrepareThreads; u0 < units || u0 == (int)blockIdx.y * kPrepareThreads; u0 += gridDim.y * kPrepareThreads) {    // queries, then keys
+      const int u = u0 + tid, h = u / kUnits, j = 4 * (u - h * kUnits), kvh = h < a.n_q_heads ? h / a.group : h - a.n_q_heads;
+      uint2 lo = make_uint2(0u, 0u), hi = lo;
+      if (u < units) {
+        const __nv_bfloat16* src = u < q_units ? q + (int64_t)h * D : kn + (int64_t)kvh * D;
+        lo = *reinterpret_cast<const uint2*>(src + j);
+        hi = *reinterpret_cast<const uint2*>(src + j + kHalf);
       }
-      *reinterpret_cast<uint2*>(dst) = make_uint2(round_bf16(rx[0], rx[1]), round_bf16(rx[2], rx[3]));
-      *reinterpret_cast<uint2*>(dst + kHalf) = make_uint2(round_bf16(ry[0], ry[1]), round_bf16(ry[2], ry[3]));
+      if (u0 == (int)blockIdx.y * kPrepareThreads) {
+        if (tid < kHalf) angle(fresh ? len : max(len - 1, 0), a.angles.inv_freq[tid], s_cos[tid], s_sin[tid]);
+        __syncthreads();
+      }
+      const float2 p0 = unpack_bf16(lo.x), p1 = unpack_bf16(lo.y), y0 = unpack_bf16(hi.x), y1 = unpack_bf16(hi.y);
+      const float4 cs = *reinterpret_cast<const float4*>(&s_cos[j]), sn = *reinterpret_cast<const float4*>(&s_sin[j]);
+      float x[4] = {turn_lo(p0.x, y0.x, cs.x, sn.x), turn_lo(p0.y, y0.y, cs.y, sn.y), turn_lo(p1.x, y1.x, cs.z, sn.z), turn_lo(p1.y, y1.y, cs.w, sn.w)};
+      float y[4] = {turn_hi(p0.x, y0.x, cs.x, sn.x), turn_hi(p0.y, y0.y, cs.y, sn.y), turn_hi(p1.x, y1.x, cs.z, sn.z), turn_hi(p1.y, y1.y, cs.w, sn.w)};
+      int shift = 0;
+      if constexpr (kE4m3) {
+        // f16 has 5 exponent bits: a query is brought to below 2 by a power of two (of up to 2^120: the rest f16 has room
+        // for), which goes into its factor. (The lanes of a head are neighbours.)
+        float top = 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) top = fmaxf(top, fmaxf(fabsf(x[e]), fabsf(y[e])));
+#pragma unroll
+        for (int o = kUnits / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        shift = min(max((int)(__float_as_uint(top) >> 23) - 127, -120), 120);
+      }
+      if (u >= units) continue;
+      if (u < q_units) {
+        if constexpr (kE4m3) {
+          const float down = __uint_as_float((uint32_t)(127 - shift) << 23);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) { x[e] *= down; y[e] *= down; }
+          if (j == 0) a.q_factor[(int64_t)i * a.n_q_heads + h] = a.scale_log2 * a.c.k_scale[kvh] * __uint_as_float((uint32_t)(127 + shift) << 23);
+        }
+        uint32_t* words = a.q + ((int64_t)i * a.n_q_heads + h) * (R::kParts * D / 2);
+        const uint32_t high[4] = {R::high(x[0], x[1]), R::high(x[2], x[3]), R::high(y[0], y[1]), R::high(y[2], y[3])};
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+          const int e = j + (n & 1) * 2 + (n >> 1) * kHalf;
+          uint32_t* word = words + R::word_thread(e) * (R::kParts * D / 8) + R::word_index(e);
+          word[0] = high[n];
+          if constexpr (R::kParts == 2) word[D / 8] = n < 2 ? R::low(x[2 * n], x[2 * n + 1], high[n]) : R::low(y[2 * n - 4], y[2 * n - 3], high[n]);
+        }
+        if (plan.n_groups > 0) {
+          __nv_bfloat16* row = plan.q_rot + (((int64_t)kvh * k + i) * a.group + h - kvh * a.group) * D + j;
+          *reinterpret_cast<uint2*>(row) = make_uint2(high[0], high[1]);
+          *reinterpret_cast<uint2*>(row + kHalf) = make_uint2(high[2], high[3]);
+        }
+      } else {
+        char* row = a.c.k_pages + to + (int64_t)kvh * a.c.head_stride + j * kSize;
+        if constexpr (kE4m3) {
+          const float per = __frcp_rn(a.c.k_scale[kvh]);
+          *reinterpret_cast<uint32_t*>(row) = round_e4m3(x[0] * per, x[1] * per, x[2] * per, x[3] * per);
+          *reinterpret_cast<uint32_t*>(row + kHalf) = round_e4m3(y[0] * per, y[1] * per, y[2] * per, y[3] * per);
+        } else {
+          *reinterpret_cast<uint2*>(row) = make_uint2(round_bf16(x[0], x[1]), round_bf16(x[2], x[3]));
+          *reinterpret_cast<uint2*>(row + D) = make_uint2(round_bf16(y[0], y[1]), round_bf16(y[2], y[3]));
+        }
+      }
+    }
+    if (to < 0) return;
+    for (int u = blockIdx.y * kPrepareThreads + tid; u < a.n_kv_heads * (D / 8); u += gridDim.y * kPrepareThreads) {
+      const int h = u / (D / 8), c = 8 * (u - h * (D / 8));
+      const uint4 v = load16(vn + (int64_t)h * D + c);
+      char* row = a.c.v_pages + to + (int64_t)h * a.c.head_stride + c * kSize;
+      if constexpr (kE4m3) {
+        float x[8];
+        widen8(v, x);
+        *reinterpret_cast<uint2*>(row) = narrow8(x, __frcp_rn(a.c.v_scale[h]));
+      } else {
+        *reinterpret_cast<uint4*>(row) = v;
+      }
     }
     return;
   }
+  if (blockIdx.y > 0) return;
   extern __shared__ int32_t s_plan[];   // group_ptr [n_groups + 1], the rows shared [n_groups], the first prompt of each group
-  __shared__ int64_t s_warp[kPlanThreads / 32];
+  __shared__ int64_t s_warp[kPrepareThreads / 32];
   __shared__ int s_bad;
   const int n = plan.n_groups;
   int32_t *s_ptr = s_plan, *s_rows = s_plan + n + 1, *s_lead = s_rows + n;
   if (tid == 0) s_bad = 0;
   __syncthreads();
-  for (int g = tid; g <= n; g += kPlanThreads) {
+  for (int g = tid; g <= n; g += kPrepareThreads) {
     const int at = plan.group_ptr[g], before = g ? plan.group_ptr[g - 1] : 0;
     if (at < before || at < 0 || at > k) s_bad = 1;
     s_ptr[g] = at;
@@ -1189,7 +1093,7 @@ shared_plan_kernel(const __grid_constant__ PlanArgs p) {
     }
     return lo;
   };
-  for (int i = tid; i < k; i += kPlanThreads) {
+  for (int i = tid; i < k; i += kPrepareThreads) {
     const int g = group_of(i), len = checked_length(a.c, a.lengths, i, fresh, nullptr);
     if (g >= 0 && len >= 0) {
       atomicMin(&s_rows[g], len);
@@ -1198,7 +1102,7 @@ shared_plan_kernel(const __grid_constant__ PlanArgs p) {
   }
   __syncthreads();
   const int page_mask = (1 << a.c.page_shift) - 1;
-  const int each = (n + kPlanThreads - 1) / kPlanThreads, g0 = min(tid * each, n), g1 = min(g0 + each, n);
+  const int each = (n + kPrepareThreads - 1) / kPrepareThreads, g0 = min(tid * each, n), g1 = min(g0 + each, n);
   int64_t units = 0, parts = 0;
   for (int g = g0; g < g1; ++g) {
     const int prompts = bad ? 0 : s_ptr[g + 1] - s_ptr[g];
@@ -1208,7 +1112,7 @@ shared_plan_kernel(const __grid_constant__ PlanArgs p) {
     units += (int64_t)tiles * ((prompts * a.group + kSharedTileRows - 1) / kSharedTileRows) * a.n_kv_heads;
     parts += (int64_t)shared_part_rows(prompts * a.group) * a.n_kv_heads;
   }
-  int64_t all, none, at = block_prefix<kPlanThreads>(units, s_warp, all), part = block_prefix<kPlanThreads>(parts, s_warp, none);
+  int64_t all, none, at = block_prefix<kPrepareThreads>(units, s_warp, all), part = block_prefix<kPrepareThreads>(parts, s_warp, none);
   for (int g = g0; g < g1; ++g) {
     const int prompts = bad ? 0 : s_ptr[g + 1] - s_ptr[g];
     SharedGroup x;
@@ -1225,7 +1129,7 @@ shared_plan_kernel(const __grid_constant__ PlanArgs p) {
   }
   if (tid == 0) *plan.units = all;
   __syncthreads();
-  for (int i = tid; i < k; i += kPlanThreads) {
+  for (int i = tid; i < k; i += kPrepareThreads) {
     const int g = group_of(i);
     plan.prompts[i] = make_int2(g >= 0 && a.lengths[i] >= 0 ? s_rows[g] : 0, g);
   }
@@ -1362,18 +1266,22 @@ cudaError_t launch_paged_decode(const PagedArgs& a, const SharedPlan& plan, cuda
   return launch_dependent(paged_combine_kernel<D, R, false>, dim3((kPieces + kJoiners - 1) / kJoiners, a.group), dim3(kCombineThreads), 0, s, a, kPieces);
 }
 
-template <int D>
-cudaError_t launch_plan(const PlanArgs& p, cudaStream_t s) {
+template <int D, bool kE4m3>
+cudaError_t launch_prepare(const PrepareArgs& p, cudaStream_t s) {
   static DeviceOnce configured;
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   if (!configured.done(dev)) {
-    e = cudaFuncSetAttribute(shared_plan_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (3 * kMaxPagedPrompts + 1) * (int)sizeof(int32_t));
+    e = cudaFuncSetAttribute(step_prepare_kernel<D, kE4m3>, cudaFuncAttributeMaxDynamicSharedMemorySize, (3 * kMaxPagedPrompts + 1) * (int)sizeof(int32_t));
     if (e != cudaSuccess) return e;
     configured.mark(dev);
   }
-  return launch_dependent(shared_plan_kernel<D>, dim3(p.a.n_prompts + 1), dim3(kPlanThreads), (3 * (size_t)p.plan.n_groups + 1) * sizeof(int32_t), s, p);
+  const int n = p.plan.n_groups;
+  // a thread for each four pairs of a head, as long as all CTAs run at once
+  const int64_t units = ((int64_t)p.a.n_q_heads + p.a.n_kv_heads) * (D / 8);
+  const int parts = (int)std::min<int64_t>((units + kPrepareThreads - 1) / kPrepareThreads, std::max(8 * kSms / p.a.n_prompts, 1));
+  return launch_dependent(step_prepare_kernel<D, kE4m3>, dim3(p.a.n_prompts + (n > 0), parts), dim3(kPrepareThreads), n > 0 ? (3 * (size_t)n + 1) * sizeof(int32_t) : 0, s, p);
 }
 
 int decode_step(const pp_attn_params* params, const pp_paged_cache* cache, const int32_t* lengths, int32_t k, const int32_t* group_ptr,
@@ -1408,6 +1316,8 @@ int decode_step(const pp_attn_params* params, const pp_paged_cache* cache, const
   a.v_new = static_cast<const __nv_bfloat16*>(v_new);
   a.o = static_cast<__nv_bfloat16*>(o);
   a.cut = reinterpret_cast<int4*>(ws + L.cut);
+  a.q = reinterpret_cast<uint32_t*>(ws + L.q);
+  a.q_factor = reinterpret_cast<float*>(ws + L.q_factor);
   a.part_ml = reinterpret_cast<float2*>(ws + L.part_ml);
   a.part_o = reinterpret_cast<float*>(ws + L.part_o);
   a.n_prompts = k;
@@ -1432,9 +1342,13 @@ int decode_step(const pp_attn_params* params, const pp_paged_cache* cache, const
     plan.group_ptr = group_ptr;
     plan.n_groups = n_groups;
     plan.n_ctas = kSms;
-    PlanArgs p{a, plan, shared_len};
-    const cudaError_t e = d == 128 ? launch_plan<128>(p, s) : launch_plan<64>(p, s);
-    if (e != cudaSuccess) return note_cuda_error((int)e, "plan kernel launch");
+  }
+  const bool e4m3 = cache->type == PP_CACHE_E4M3;
+  const PrepareArgs p{a, plan, shared_len};
+  const cudaError_t prepared = d == 128 ? (e4m3 ? launch_prepare<128, true>(p, s) : launch_prepare<128, false>(p, s))
+                                        : (e4m3 ? launch_prepare<64, true>(p, s) : launch_prepare<64, false>(p, s));
+  if (prepared != cudaSuccess) return note_cuda_error((int)prepared, "step preparation launch");
+  if (n_groups > 0) {
     if ((st = launch_shared_attention(*params, a.c, plan, k, a.scale_log2, device_status, s)) != PP_OK) return st;
     const int64_t heads = (int64_t)k * params->n_q_heads;
     const bool across = heads <= 8 * kSms;          // as long as a CTA for each runs at once
@@ -1444,7 +1358,6 @@ int decode_step(const pp_attn_params* params, const pp_paged_cache* cache, const
                                         : (across ? join(shared_join_kernel<64, true>) : join(shared_join_kernel<64, false>));
     if (joined != cudaSuccess) return note_cuda_error((int)joined, "join kernel launch");
   }
-  const bool e4m3 = cache->type == PP_CACHE_E4M3;
   const cudaError_t e = d == 128 ? (e4m3 ? launch_paged_decode<128, true>(a, plan, s) : launch_paged_decode<128, false>(a, plan, s))
                                  : (e4m3 ? launch_paged_decode<64, true>(a, plan, s) : launch_paged_decode<64, false>(a, plan, s));
   return e == cudaSuccess ? PP_OK : note_cuda_error((int)e, "paged generation step launch");
@@ -1468,6 +1381,8 @@ PagedWorkspace paged_workspace(const pp_attn_params& p, int32_t k, int32_t n_gro
   };
   const size_t parts = 2 * (size_t)kMostPieces * (p.n_q_heads / p.n_kv_heads);
   L.cut = take((size_t)kMostPieces * sizeof(int4));
+  L.q = take((size_t)k * p.n_q_heads * p.head_dim * sizeof(uint32_t));
+  L.q_factor = take((size_t)k * p.n_q_heads * sizeof(float));
   L.part_ml = take(parts * sizeof(float2));
   L.part_o = take(parts * p.head_dim * sizeof(float));
   if (n_groups > 0) {

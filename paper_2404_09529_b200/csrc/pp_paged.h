@@ -55,6 +55,7 @@ RopeAngles rope_angles(float base, int32_t head_dim);
 // its rows, or two where it has so few rows that both tiles of the kernel work on them (first all those of one, then of the other).
 struct PagedWorkspace {
   size_t cut;                           // int4 for each piece of the line of own rows
+  size_t q, q_factor;                   // the queries as the products take them
   size_t part_ml, part_o;               // float2, float[D]
   // with shared rows only
   size_t units;                         // int64: units in all
