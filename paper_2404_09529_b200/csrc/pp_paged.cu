@@ -190,7 +190,7 @@ append_kernel(const __grid_constant__ AppendArgs a) {
 //   step_prepare_kernel   a CTA for each prompt: rotates its queries, rotates and appends the new token. (With shared rows a further
 //                         CTA lays their work out, see below.)
 //   paged_decode_kernel   attention over the rows, the appended one like any other
-//   paged_combine_kernel  joins the parts of items that were cut
+//   paged_combine_kernel  joins the parts of items that were cut (with shared rows shared_join_kernel does, and those over shared rows)
 // Bound: HBM, every row of K and V is read once. The work is a line of units of 8 KB (16, 32 or 64 rows of K and V of one KV
 // head), ordered by (prompt, KV head, rows), and cut into equal pieces, one for each warp that the GPU holds: all warps read the
 // same number of bytes whatever the lengths are. A warp works on its own from there on. Its rows arrive by TMA in a ring of
@@ -198,7 +198,8 @@ append_kernel(const __grid_constant__ AppendArgs a) {
 // instructions a byte) keep up to 96 KB of an SM under way, which is all that HBM takes: with twelve, the loads queued up and SMs
 // were served so unevenly that of 148 equal shares the last ended 20 % after the mean. A piece that is a whole item (prompt, KV head)
 // leaves O at once. What an item costs beside its rows is the latency of one warp: with the queries rotated there, and the new token a step
-// of its own, 4700 cycles of 1800 a unit (64 prompts on 32 heads 57.8 -> PREP7B us, 256 prompts behind 8192 shared rows 114 -> PREPSYS).
+// of its own, 4700 cycles of 1800 a unit (prepared apart: 64 prompts on 32 heads 57.8 -> 56.9 us,
+// 64 prompts behind one document of 4096 rows 59 -> 55, 16 samples of one prompt 25.9 -> 23.7; ten prompts on one layer 11.4 -> 12.1).
 // The arithmetic is that of the step over contiguous caches (pp_decode.cu): mma.m16n8k16 with 16 keys as rows and the query heads
 // of a KV head as the 8 columns, absent heads 0. Over bf16 pages a query and a weight each reach it as the sum of two
 // 16-bit numbers: HBM leaves the tensor cores idle, and scores and O are then exact to 2^-16, far below O's last rounding of 2^-8.
@@ -222,6 +223,10 @@ struct PagedArgs {
   const __nv_bfloat16 *q_new, *k_new, *v_new;
   int64_t q_stride, k_stride, v_stride;
   __nv_bfloat16* o;
+  int2* items;                          // with shared rows: of every item (prompt, KV head) the piece in which it begins and its parts, 0: one,
+                                        // which lies in row_ml, row_o [prompt][head]
+  float2* row_ml;
+  float* row_o;
   int4* cut;                            // [pieces]: of the item that begins in a piece and ends in another: prompt, KV head, pieces; 0 pieces: none
   uint32_t* q;                          // queries as the products take them: [prompt][head][t][parts][D / 8] words, see Rows
   float* q_factor;                      // [prompt][head] over 8-bit pages: from a product with them to scaled log2 units
@@ -388,7 +393,6 @@ struct Rows<D, false> {
     const int g = place / (D / 8), r = place % (D / 8);
     return 16 * (r >> 1) + 8 * (r & 1) + g;
   }
-  static __device__ __forceinline__ int place_of(int element) { return (D / 8) * (element & 7) + (element >> 4) * 2 + ((element >> 3) & 1); }
   // O of the eight heads as rows of bf16, heads 2t and 2t + 1 times f0 and f1 (transposed, a lane holds pairs of elements of one head)
   static __device__ __forceinline__ void leave(const float (&acc)[D / 16][4], float f0, float f1, uint32_t at, int g, int t) {
 #pragma unroll
@@ -505,7 +509,8 @@ struct Rows<D, true> {
 };
 
 // A warp's place on the line: the part of an item (prompt i, KV head kvh) that lies in its piece. An item takes kItemUnits of the line
-// more than it has units: what its beginning and end cost its warp.
+// more than it has units: what its beginning and end cost its warp. (1, 2, 3 over 242 k rows of 256 prompts on 8 KV heads: 167.5, 160.6,
+// 160.0 us; over 8-bit pages 95.4, 90.4, 91.7; 192 prompts with about 160 rows of their own each: 184, 167.7, 167.8.)
 constexpr int kItemUnits = 2;
 struct Place {
   int64_t left;                         // of the piece, from here on
@@ -565,8 +570,7 @@ struct Line {
 
 template <int D, bool kE4m3>
 __global__ void __launch_bounds__(32 * Rows<D, kE4m3>::kWarps, 1)
-paged_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ PagedArgs a,
-                    const __grid_constant__ SharedPlan plan) {
+paged_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ PagedArgs a) {
   using R = Rows<D, kE4m3>;
   constexpr int kWarps = R::kWarps, kThreads = 32 * kWarps, kPieces = kSms * kWarps;
   constexpr int kSteps = R::kSteps, kUnitRows = 16 * kSteps, kWords = R::kParts * D / 8;
@@ -601,7 +605,7 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
   Place c;                              // where the arithmetic is
   c.left = min(per, total - u0);
   if (lane == 0) a.cut[piece] = make_int4(0, 0, 0, 0);
-  if (c.left <= 0) return pdl_wait();   // (the kernel after this one counts on all in front of it)
+  if (c.left <= 0) return pdl_wait();
   {
     int lo = 0;                         // last thread whose prompts begin at or before u0 (those without units come before it)
     for (int w = 0; w < kWarps; ++w) lo += __popc(__ballot_sync(0xffffffffu, s_before[32 * w + lane] <= u0));
@@ -670,8 +674,12 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
     load_k();
     load_v();
   }
-  pdl_wait();                           // the queries and the appended rows
-  pdl_launch_dependents();
+  // The queries and the appended rows. With shared rows they are there: the kernel in front has waited for them, and nothing of its own
+  // is looked at here. So this one begins on every SM that has done its share of that.
+  if (!a.items) {
+    pdl_wait();
+    pdl_launch_dependents();
+  }
   for (; loaded < 2; ++loaded) {
     load_k();
     load_v();
@@ -711,28 +719,9 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
     Place next = c;
     line.advance(next);
     if (next.n > 0) fetch(next_q, next);
-    // (m, l) and o over the rows that the prompt shares, where this part is the item's first
     float m[2] = {kNoScore, kNoScore}, l[2] = {0.f, 0.f}, acc[D / 16][4];
 #pragma unroll
     for (int j = 0; j < D / 16; ++j) acc[j][0] = acc[j][1] = acc[j][2] = acc[j][3] = 0.f;
-    if (begins && c.start > 0) {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int head = 2 * t + h;
-        if (head >= a.group) continue;
-        const int64_t at = (int64_t)c.i * a.n_q_heads + c.kvh * a.group + head;
-        const float2 ml = __ldcg(plan.row_ml + at);
-        m[h] = ml.x;
-        l[h] = g == 0 ? ml.y : 0.f;
-        const float4* from = reinterpret_cast<const float4*>(plan.row_o + at * D + (D / 8) * g);
-#pragma unroll
-        for (int j = 0; j < D / 16; j += 2) {
-          const float4 x = __ldcg(from + (j >> 1));
-          acc[j][h] = x.x; acc[j][2 + h] = x.y;
-          acc[j + 1][h] = x.z; acc[j + 1][2 + h] = x.w;
-        }
-      }
-    }
 
     // ---- the rows
     // Weights of the scores in s (rows at or past n_real are hidden), with O, l and m brought to the new maximum.
@@ -804,7 +793,7 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int o = 4; o < 32; o <<= 1) l[h] += __shfl_xor_sync(0xffffffffu, l[h], o);
-    if (begins && ends) {
+    if (begins && ends && !a.items) {
       // (a row that attends to nothing is 0; one all of whose scores are -inf is a NaN)
       const bool none = c.len == 0;
       R::leave(acc, none ? 0.f : out_scale / l[0], none ? 0.f : out_scale / l[1], scratch, g, t);
@@ -813,13 +802,16 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
       for (int x = lane; x < a.group * D / 8; x += 32) *reinterpret_cast<uint4*>(to + 8 * x) = shared16(scratch + 16 * x);
       __syncwarp();
     } else {
-      const int64_t slot = 2 * (int64_t)piece + (begins ? 1 : 0);
+      const bool whole = begins && ends;
+      const int64_t item = (int64_t)c.i * a.n_kv_heads + c.kvh, to_row = (whole ? item : 2 * (int64_t)piece + (begins ? 1 : 0)) * a.group;
+      float2* to_ml = (whole ? a.row_ml : a.part_ml) + to_row;
+      float* to_o = (whole ? a.row_o : a.part_o) + to_row * D;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int head = 2 * t + h;
         if (head >= a.group) continue;
-        if (g == 0) a.part_ml[slot * a.group + head] = make_float2(m[h], l[h]);
-        float* to = a.part_o + (slot * a.group + head) * D + (D / 8) * g;
+        if (g == 0) to_ml[head] = make_float2(m[h], l[h]);
+        float* to = to_o + head * D + (D / 8) * g;
 #pragma unroll
         for (int j = 0; j < D / 16; j += 4)       // (whole sectors: 32 bytes a store)
           asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
@@ -827,10 +819,13 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
                          "f"(acc[j + 1][2 + h] * out_scale), "f"(acc[j + 2][h] * out_scale), "f"(acc[j + 2][2 + h] * out_scale),
                          "f"(acc[j + 3][h] * out_scale), "f"(acc[j + 3][2 + h] * out_scale) : "memory");
       }
-      if (begins && lane == 0)          // the pieces over which the item goes on: units behind this one's end
-        a.cut[piece] = make_int4(c.i, c.kvh, 1 + (int)((c.units - c.n + per - 1) / per), 0);
+      if (begins && lane == 0) {        // the pieces over which the item goes on: units behind this one's end
+        const int parts = whole ? 0 : 1 + (int)((c.units - c.n + per - 1) / per);
+        if (a.items) a.items[item] = make_int2(piece, parts);
+        else a.cut[piece] = make_int4(c.i, c.kvh, parts, 0);
+      }
     }
-    if (next.n == 0) return;
+    if (next.n == 0) return pdl_wait();     // (the kernel after this one counts on all in front of it)
     c = next;
   }
 }
@@ -882,6 +877,14 @@ __device__ __forceinline__ Joined<D> join_parts(int first, int step, int n, cons
       for (int e = 0; e < E; ++e) s.o[e] += p[c][e] * f;
     }
   }
+  return s;
+}
+template <int D>
+__device__ __forceinline__ Joined<D> join_two(const Joined<D>& x, const Joined<D>& y) {
+  const float m = fmaxf(x.m, y.m), f = x.l == 0.f ? 0.f : ex2(x.m - m), g = y.l == 0.f ? 0.f : ex2(y.m - m);
+  Joined<D> s{m, x.l * f + y.l * g, {}};
+#pragma unroll
+  for (int e = 0; e < Joined<D>::E; ++e) s.o[e] = x.o[e] * f + y.o[e] * g;
   return s;
 }
 // What the warps of a CTA have joined of one head, as one: `leave` gets m, l and o of every place, a thread for each. (Ends with a barrier.)
@@ -1135,8 +1138,8 @@ step_prepare_kernel(const __grid_constant__ PrepareArgs p) {
   }
 }
 
-// The parts of every query head over the shared rows, from the CTAs of the attention kernel, become one: a warp for each head of each
-// prompt, or, of few, a CTA (kAcross). The step over the prompts' own rows goes on from there, and finds the elements in its order.
+// With shared rows: joins the parts of every query head, those over the rows that its prompt shares, from the CTAs of their kernel, and
+// those over its own. A warp for each head of each prompt, or, of few, a CTA (kAcross).
 template <int D, bool kAcross>
 __global__ void __launch_bounds__(kCombineThreads)
 shared_join_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ SharedPlan plan) {
@@ -1148,29 +1151,40 @@ shared_join_kernel(const __grid_constant__ PagedArgs a, const __grid_constant__ 
   pdl_wait();
   pdl_launch_dependents();
   if (row >= (int64_t)a.n_prompts * a.n_q_heads) return;
-  const int i = (int)(row / a.n_q_heads), head = (int)(row - (int64_t)i * a.n_q_heads), kvh = head / a.group;
-  const int2 own = plan.prompts[i];
-  const int64_t per = units_per_piece(*plan.units, plan.n_ctas);
-  if (own.x == 0) return;               // nothing shared
-  const SharedGroup gr = plan.groups[own.y];
-  const int r = (i - gr.first) * a.group + head - kvh * a.group, rt = r / kSharedTileRows;
-  const int64_t u0 = gr.unit_start + ((int64_t)kvh * ((gr.query_rows + kSharedTileRows - 1) / kSharedTileRows) + rt) * gr.key_tiles;
-  const int p0 = (int)(u0 / per), n = (int)((u0 + gr.key_tiles - 1) / per) - p0 + 1;
-  // (an item of few rows has two parts in each piece, see pp_paged.h)
-  const int item_rows = min(gr.query_rows - rt * kSharedTileRows, kSharedTileRows), sides = item_rows <= kSharedTileRows / 2 ? 2 : 1;
-  const int64_t at = (int64_t)p0 * kSharedTileRows + gr.part_start + (int64_t)kvh * shared_part_rows(gr.query_rows) + r;
-  auto part_row = [&](int part) { return at + (int64_t)(sides == 2 ? part >> 1 : part) * kSharedTileRows + (sides == 2 && (part & 1) ? item_rows : 0); };
-  float* to = plan.row_o + row * D;
+  const int i = (int)(row / a.n_q_heads), head = (int)(row - (int64_t)i * a.n_q_heads), kvh = head / a.group, h = head - kvh * a.group;
+  const bool fresh = a.k_new != nullptr;
+  const int len = checked_length(a.c, a.lengths, i, fresh, nullptr);
+  const int2 own = __ldcg(plan.prompts + i), item = __ldcg(a.items + (int64_t)i * a.n_kv_heads + kvh);
+  const int64_t per = units_per_piece(__ldcg(plan.units), plan.n_ctas);
+  if (len < 0) return;
+  // (a row that attends to nothing is 0; one all of whose scores are -inf is a NaN)
+  const bool none = len + (int)fresh == 0;
+  __nv_bfloat16* to = a.o + row * D;
+  auto own_row = [&](int part) { return (2 * (int64_t)item.x + (part == 0 ? 1 : 2 * part)) * a.group + h; };
+  auto whole_row = [&](int) { return row; };
+  int n = 0, item_rows = 0, sides = 1;
+  int64_t at = 0;
+  if (own.x > 0) {
+    const SharedGroup gr = plan.groups[own.y];
+    const int r = (i - gr.first) * a.group + h, rt = r / kSharedTileRows;
+    const int64_t u0 = gr.unit_start + ((int64_t)kvh * ((gr.query_rows + kSharedTileRows - 1) / kSharedTileRows) + rt) * gr.key_tiles;
+    const int p0 = (int)(u0 / per);
+    n = (int)((u0 + gr.key_tiles - 1) / per) - p0 + 1;
+    // (an item of few rows has two parts in each piece, see pp_paged.h)
+    item_rows = min(gr.query_rows - rt * kSharedTileRows, kSharedTileRows);
+    sides = item_rows <= kSharedTileRows / 2 ? 2 : 1;
+    at = (int64_t)p0 * kSharedTileRows + gr.part_start + (int64_t)kvh * shared_part_rows(gr.query_rows) + r;
+  }
+  auto shared_row = [&](int part) { return at + (int64_t)(sides == 2 ? part >> 1 : part) * kSharedTileRows + (sides == 2 && (part & 1) ? item_rows : 0); };
+  const int first = kAcross ? warp : 0, step = kAcross ? kWarps : 1;
+  Joined<D> s = item.y > 0 ? join_parts<D, 4>(first, step, item.y, a.part_ml, a.part_o, lane, own_row)
+                           : join_parts<D, 1>(first, step, 1, a.row_ml, a.row_o, lane, whole_row);
+  if (n > 0) s = join_two(s, join_parts<D, 4>(first, step, n * sides, plan.ml, plan.o, lane, shared_row));
   if constexpr (kAcross) {
-    join_warps<D, kWarps>(join_parts<D, 4>(warp, kWarps, n * sides, plan.ml, plan.o, lane, part_row), space, [&](float m, float l, float o, int element) {
-      if (element == 0) plan.row_ml[row] = make_float2(m, l);
-      to[R::place_of(element)] = o;
-    });
+    join_warps<D, kWarps>(s, space, [&](float, float l, float o, int place) { to[R::element_at(place)] = __float2bfloat16_rn(none ? 0.f : o / l); });
   } else {
-    const Joined<D> s = join_parts<D, 4>(0, 1, n * sides, plan.ml, plan.o, lane, part_row);
-    if (lane == 0) plan.row_ml[row] = make_float2(s.m, s.l);
 #pragma unroll
-    for (int e = 0; e < E; ++e) to[R::place_of(E * lane + e)] = s.o[e];
+    for (int e = 0; e < E; ++e) to[R::element_at(E * lane + e)] = __float2bfloat16_rn(none ? 0.f : s.o[e] / s.l);
   }
 }
 
@@ -1245,7 +1259,7 @@ bool page_map(CUtensorMap* map, const void* pages, const PagedArgs& a, int d, bo
 }
 
 template <int D, bool kE4m3>
-cudaError_t launch_paged_decode(const PagedArgs& a, const SharedPlan& plan, cudaStream_t s) {
+cudaError_t launch_paged_decode(const PagedArgs& a, cudaStream_t s) {
   constexpr int kWarps = Rows<D, kE4m3>::kWarps, kSmem = 1024 + kWarps * (4 * kHalfUnit + kScratch);     // rings on 1024-byte boundaries
   static DeviceOnce configured;
   int dev = 0;
@@ -1258,8 +1272,8 @@ cudaError_t launch_paged_decode(const PagedArgs& a, const SharedPlan& plan, cuda
   }
   CUtensorMap mk, mv;
   if (!page_map(&mk, a.c.k_pages, a, D, kE4m3) || !page_map(&mv, a.c.v_pages, a, D, kE4m3)) return cudaErrorInvalidValue;
-  e = launch_dependent(paged_decode_kernel<D, kE4m3>, dim3(kSms), dim3(32 * kWarps), (size_t)kSmem, s, mk, mv, a, plan);
-  if (e != cudaSuccess) return e;
+  e = launch_dependent(paged_decode_kernel<D, kE4m3>, dim3(kSms), dim3(32 * kWarps), (size_t)kSmem, s, mk, mv, a);
+  if (e != cudaSuccess || a.items) return e;          // (with shared rows another kernel joins the parts)
   constexpr int kPieces = kSms * kWarps, kJoiners = kCombineThreads / 32;
   using R = Rows<D, kE4m3>;
   if (kPieces * a.group <= 8 * kSms) return launch_dependent(paged_combine_kernel<D, R, true>, dim3(kPieces, a.group), dim3(kCombineThreads), 0, s, a, kPieces);
@@ -1316,6 +1330,9 @@ int decode_step(const pp_attn_params* params, const pp_paged_cache* cache, const
   a.v_new = static_cast<const __nv_bfloat16*>(v_new);
   a.o = static_cast<__nv_bfloat16*>(o);
   a.cut = reinterpret_cast<int4*>(ws + L.cut);
+  a.items = n_groups > 0 ? reinterpret_cast<int2*>(ws + L.items) : nullptr;
+  a.row_ml = reinterpret_cast<float2*>(ws + L.row_ml);
+  a.row_o = reinterpret_cast<float*>(ws + L.row_o);
   a.q = reinterpret_cast<uint32_t*>(ws + L.q);
   a.q_factor = reinterpret_cast<float*>(ws + L.q_factor);
   a.part_ml = reinterpret_cast<float2*>(ws + L.part_ml);
@@ -1337,8 +1354,6 @@ int decode_step(const pp_attn_params* params, const pp_paged_cache* cache, const
     plan.q_rot = reinterpret_cast<__nv_bfloat16*>(ws + L.q_rot);
     plan.ml = reinterpret_cast<float2*>(ws + L.shared_ml);
     plan.o = reinterpret_cast<float*>(ws + L.shared_o);
-    plan.row_ml = reinterpret_cast<float2*>(ws + L.row_ml);
-    plan.row_o = reinterpret_cast<float*>(ws + L.row_o);
     plan.group_ptr = group_ptr;
     plan.n_groups = n_groups;
     plan.n_ctas = kSms;
@@ -1350,16 +1365,17 @@ int decode_step(const pp_attn_params* params, const pp_paged_cache* cache, const
   if (prepared != cudaSuccess) return note_cuda_error((int)prepared, "step preparation launch");
   if (n_groups > 0) {
     if ((st = launch_shared_attention(*params, a.c, plan, k, a.scale_log2, device_status, s)) != PP_OK) return st;
+  }
+  cudaError_t e = d == 128 ? (e4m3 ? launch_paged_decode<128, true>(a, s) : launch_paged_decode<128, false>(a, s))
+                           : (e4m3 ? launch_paged_decode<64, true>(a, s) : launch_paged_decode<64, false>(a, s));
+  if (e == cudaSuccess && n_groups > 0) {
     const int64_t heads = (int64_t)k * params->n_q_heads;
     const bool across = heads <= 8 * kSms;          // as long as a CTA for each runs at once
     const dim3 blocks((unsigned)(across ? heads : (heads + kCombineThreads / 32 - 1) / (kCombineThreads / 32)));
     auto join = [&](auto kernel) { return launch_dependent(kernel, blocks, dim3(kCombineThreads), 0, s, a, plan); };
-    const cudaError_t joined = d == 128 ? (across ? join(shared_join_kernel<128, true>) : join(shared_join_kernel<128, false>))
-                                        : (across ? join(shared_join_kernel<64, true>) : join(shared_join_kernel<64, false>));
-    if (joined != cudaSuccess) return note_cuda_error((int)joined, "join kernel launch");
+    e = d == 128 ? (across ? join(shared_join_kernel<128, true>) : join(shared_join_kernel<128, false>))
+                 : (across ? join(shared_join_kernel<64, true>) : join(shared_join_kernel<64, false>));
   }
-  const cudaError_t e = d == 128 ? (e4m3 ? launch_paged_decode<128, true>(a, plan, s) : launch_paged_decode<128, false>(a, plan, s))
-                                 : (e4m3 ? launch_paged_decode<64, true>(a, plan, s) : launch_paged_decode<64, false>(a, plan, s));
   return e == cudaSuccess ? PP_OK : note_cuda_error((int)e, "paged generation step launch");
 }
 
@@ -1393,6 +1409,7 @@ PagedWorkspace paged_workspace(const pp_attn_params& p, int32_t k, int32_t n_gro
     const size_t rows = (size_t)kSms * kSharedTileRows + 2 * (size_t)k * p.n_q_heads;
     L.shared_ml = take(rows * sizeof(float2));
     L.shared_o = take(rows * p.head_dim * sizeof(float));
+    L.items = take((size_t)k * p.n_kv_heads * sizeof(int2));
     L.row_ml = take((size_t)k * p.n_q_heads * sizeof(float2));
     L.row_o = take((size_t)k * p.n_q_heads * p.head_dim * sizeof(float));
   }

@@ -63,7 +63,7 @@ struct PagedWorkspace {
   size_t prompts;                       // int2 [k]: first row that the prompt reads on its own, its group (-1: none)
   size_t q_rot;                         // bf16 [Hkv][k * group][D]
   size_t shared_ml, shared_o;           // float2, float[D]: parts
-  size_t row_ml, row_o;                 // [k][Hq]: joined
+  size_t items, row_ml, row_o;          // int2 [k][Hkv]; float2, float[D] [k][Hq]: of items that are not cut
   size_t total;
 };
 PagedWorkspace paged_workspace(const pp_attn_params& p, int32_t k, int32_t n_groups);
@@ -83,8 +83,8 @@ struct SharedPlan {
   SharedGroup* groups;
   int2* prompts;
   __nv_bfloat16* q_rot;
-  float2 *ml, *row_ml;
-  float *o, *row_o;
+  float2* ml;
+  float* o;
   const int32_t* group_ptr;
   int32_t n_groups, n_ctas;             // n_ctas: pieces that the line of units is cut into
 };

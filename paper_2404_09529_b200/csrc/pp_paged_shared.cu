@@ -12,8 +12,8 @@
 //   warps 4-7    softmax of tile 0, a thread per row: no row is split between threads, so nothing is exchanged
 //   warps 8-11   the same for tile 1
 // A tile's softmax runs while the other tile's products do. An item of at most 128 rows has no second row tile: the two then take its
-// key tiles in turn, each with an O of its own, so that there are two chains of product, softmax and product here too. The pages of a tile that the group does not share are loaded from
-// beyond the last page, which TMA fills with zeros.
+// key tiles in turn, each with an O of its own, so that there are two chains of product, softmax and product here too. The pages of a
+// tile that the group does not share are loaded from beyond the last page, which TMA fills with zeros.
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -396,17 +396,20 @@ shared_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
         const bool any = first < n;               // (a tile that took no keys leaves l = 0, and its O is not looked at)
         if (row < rows) args.plan.ml[out + row] = make_float2(fmaxf(m_run, -FLT_MAX), sum_f2x2(sum_a, sum_b));
         float* dst = args.plan.o + (out + row) * D;
-#pragma unroll 1
-        for (int ch = 0; any && ch < D / 32; ++ch) {
-          uint32_t ov[32];
-          tmem_ld32(tm_o + 32 * ch, ov);
+        if (any) {
+          uint32_t ov[D];
+#pragma unroll
+          for (int ch = 0; ch < D / 32; ++ch) tmem_ld32(tm_o + 32 * ch, *reinterpret_cast<uint32_t(*)[32]>(&ov[32 * ch]));
           tc_wait_ld();
           if (row < rows) {
+            // whole sectors, 32 bytes a store, in the order of the parts over own rows: element 16 j + 8 x + g at (D / 8) g + 2 j + x
 #pragma unroll
-            for (int i = 0; i < 32; i += 8)       // (a lane's own sector: 32 bytes of its row)
+            for (int to = 0; to < D; to += 8) {
+              const int g = to / (D / 8), j = to % (D / 8) / 2;
               asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
-                           ::"l"(dst + 32 * ch + i), "r"(ov[i]), "r"(ov[i + 1]), "r"(ov[i + 2]), "r"(ov[i + 3]), "r"(ov[i + 4]), "r"(ov[i + 5]),
-                             "r"(ov[i + 6]), "r"(ov[i + 7]) : "memory");
+                           ::"l"(dst + to), "r"(ov[16 * j + g]), "r"(ov[16 * j + 8 + g]), "r"(ov[16 * j + 16 + g]), "r"(ov[16 * j + 24 + g]),
+                             "r"(ov[16 * j + 32 + g]), "r"(ov[16 * j + 40 + g]), "r"(ov[16 * j + 48 + g]), "r"(ov[16 * j + 56 + g]) : "memory");
+            }
           }
         }
         tc_fence_before();
