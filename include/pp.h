@@ -364,8 +364,9 @@ int pp_paged_append(const pp_attn_params* params, const pp_paged_cache* cache, c
  *   device_status device int32 or NULL, see PP_PAGED_*; the caller zeroes and reads it
  * No host memory is read after the call and nothing depends on the lengths but what the kernels do: the call can be
  * captured once and replayed for every step. Two prompts may share pages only below both of their lengths.
- * Arithmetic: scores, probabilities and sums in fp32 (the rotated query and the probabilities reach the tensor cores as
- * the sum of two or three 16-bit numbers), one rounding of O to bf16. Cached values may be infinite or NaN; rows that a
+ * Arithmetic: scores, probabilities and sums in fp32, one rounding of O to bf16. Over bf16 pages the rotated query and the
+ * probabilities reach the tensor cores as the sum of two bf16 numbers each (2^-16), over 8-bit pages as one f16 number (2^-12; a
+ * query times a power of two that brings it below 2). Cached values may be infinite or NaN; rows that a
  * prompt does not have may hold anything. Asynchronous on `stream`.
  * Errors: PP_ERR_INVALID_ARG, PP_ERR_UNSUPPORTED (head_dim, more than 8 query heads per KV head, page_size, type, device),
  * PP_ERR_TOO_LARGE (k > 8192), PP_ERR_ALIGNMENT, PP_ERR_BUFFER_TOO_SMALL, PP_ERR_CUDA.

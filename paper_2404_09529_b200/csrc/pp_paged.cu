@@ -686,10 +686,12 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
   }
 
   uint32_t stage = 0, phase = 0;
-  // A wait gave up: loads of this warp may still be in flight. They get time to land before shared memory is handed back.
+  // A wait gave up: loads of this warp may still be in flight. They get time to land before shared memory is handed back. (And the
+  // end of this kernel still says that those in front of it have ended.)
   auto settle = [&]() {
     const unsigned long long t0 = global_ns();
     while (global_ns() - t0 < 100000ull) {}
+    pdl_wait();
   };
   // The queries of an item, of head g (zeros for absent heads), and of heads 2t and 2t + 1 the factor of their scores.
   struct Queries { uint32_t w[kWords]; float factor[2]; };

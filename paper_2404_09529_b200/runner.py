@@ -295,7 +295,7 @@ class PagedCaches:
                  k_scale: torch.Tensor | None = None, v_scale: torch.Tensor | None = None) -> "PagedCaches":
         """Pools of n_pages zeroed pages and an empty table for n_prompts prompts of up to max_rows rows."""
         shape = (n_pages, page_size, n_kv_heads, head_dim) if rows_first else (n_pages, n_kv_heads, page_size, head_dim)
-        pools = [torch.zeros(shape, dtype=torch.bfloat16, device=device).to(dtype) for _ in range(2)]
+        pools = [torch.zeros(shape, dtype=torch.uint8 if dtype.itemsize == 1 else torch.bfloat16, device=device).view(dtype) for _ in range(2)]
         table = torch.full((n_prompts, -(-max_rows // page_size)), -1, dtype=torch.int32, device=device)
         self = cls(*pools, table, rows_first, k_scale, v_scale)
         self._table = np.full(tuple(table.shape), -1, dtype=np.int32)     # what the device table holds
@@ -304,16 +304,18 @@ class PagedCaches:
         self._free = list(range(n_pages - 1, -1, -1))
         return self
 
-    def _owned(self) -> None:
+    def _owned(self, *prompts: int) -> None:
         if self._count is None:
             raise ValueError("the table of these caches belongs to the caller")
+        if not all(0 <= p < self.n_prompts for p in prompts):
+            raise IndexError(f"prompts are 0 .. {self.n_prompts - 1}")
 
     def _write_row(self, prompt: int) -> None:
         self.page_table[prompt].copy_(torch.from_numpy(self._table[prompt].copy()))
 
     def reserve(self, prompt: int, rows: int) -> None:
         """Pages for rows 0 .. rows - 1 of a prompt, in addition to those it has."""
-        self._owned()
+        self._owned(prompt)
         have, want = int(self._count[prompt]), -(-rows // self.page_size)
         if want > self._table.shape[1]:
             raise ValueError(f"{rows} rows do not fit the prompt's row of the page table")
@@ -330,8 +332,8 @@ class PagedCaches:
     def share(self, source: int, prompt: int, rows: int) -> int:
         """Gives an empty prompt the pages of `source` that lie wholly within its first `rows` rows. Returns how many rows those
         are; the rows behind them are the prompt's own (append them again)."""
-        self._owned()
-        n = rows // self.page_size
+        self._owned(source, prompt)
+        n = max(rows, 0) // self.page_size
         if self._count[prompt]:
             raise ValueError("the prompt has pages already")
         if n > self._count[source]:
@@ -344,7 +346,7 @@ class PagedCaches:
 
     def release(self, prompt: int) -> None:
         """Gives a prompt's pages back, those at least that no other prompt has."""
-        self._owned()
+        self._owned(prompt)
         pages = self._table[prompt, :self._count[prompt]]
         self._users[pages] -= 1
         self._free.extend(int(p) for p in pages if self._users[p] == 0)
@@ -442,6 +444,9 @@ class PagedDecoder:
                 raise ValueError("no generation step for these shapes")
             self._sizes[(k, n_groups)] = need
         if not self._workspaces or self._workspaces[-1][1] < need:
+            # (twice the last one at least: all that are kept take no more than the last one again, however the prompts grow in number)
+            if self._workspaces:
+                need = max(need, 2 * self._workspaces[-1][1])
             self._workspaces.append((torch.empty(need, dtype=torch.uint8, device=self.caches.device), need))
         return self._workspaces[-1]
 
@@ -470,6 +475,8 @@ class PagedDecoder:
             n_groups = c.check_ints(shared, "shared_len")
             if c.check_ints(ptr, "group_ptr") != n_groups + 1:
                 raise ValueError("groups: group_ptr has one entry more than shared_len")
+            if n_groups == 0:
+                groups = None
         with on_device(c.device):
             if groups is None:
                 ws, size = self._workspace(n, 0)

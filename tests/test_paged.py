@@ -278,7 +278,9 @@ def test_step_refusals():
 
 def test_workspace_bytes():
     ask = pp.pp_paged_decode_workspace_bytes
-    assert ask(_params(), 1) > 0 and ask(_params(), 8192) == ask(_params(), 1)
+    p = _params()
+    # parts of what is cut, whose number does not depend on k, and the prepared queries: a word an element, a factor a head
+    assert 0 < ask(p, 1) and abs(ask(p, 8192) - ask(p, 1) - 8191 * p.n_q_heads * (p.head_dim + 1) * 4) < 512      # (each on a boundary of 256)
     assert ask(_params(), 4, 4) > ask(_params(), 4, 1) - 1 > ask(_params(), 4)
     assert [ask(_params(), k, g) for k, g in ((0, 0), (8193, 0), (4, 5), (4, -1))] == [0] * 4
     assert ask(_params(hq=6), 4) == 0 and ask(_params(d=80), 4) == 0
@@ -867,3 +869,120 @@ def test_samples_of_one_prompt():
         e = (out.float() - alone.float()).abs()
         assert float(e.max()) <= MAX_ABS_TOL and float(e.mean()) <= MEAN_ABS_TOL
     assert dec.device_status() == 0 and int(caches.status) == 0
+
+
+# ------------------------------------------------------------------------------------------
+# Calls at the edges
+# ------------------------------------------------------------------------------------------
+def test_pages_of_prompts_that_there_are_not():
+    c = PagedCaches.allocate(3, 8, 64, 1, 64, page_size=16, device="cpu")
+    c.reserve(0, 40)
+    for call in (lambda: c.reserve(-1, 16), lambda: c.reserve(3, 16), lambda: c.share(-3, 1, 16), lambda: c.share(0, 3, 16), lambda: c.release(-1)):
+        with pytest.raises(IndexError):
+            call()
+    before = c.page_table.clone()
+    assert c.share(0, 1, -20) == 0 and torch.equal(c.page_table, before)
+    c.reserve(1, 16)                                   # the prompt was left empty, and the free pages as they were
+    assert int(c.page_table[1][0]) not in c.page_table[0][:3].tolist()
+
+
+def test_pools_are_allocated_as_zeros():
+    for dtype in (BF16, E4M3):
+        scales = {} if dtype is BF16 else {"k_scale": torch.ones(2), "v_scale": torch.ones(2)}
+        c = PagedCaches.allocate(1, 3, 40, 2, 64, page_size=16, dtype=dtype, device="cpu", **scales)
+        assert c.k_pages.dtype is dtype and c.k_pages.shape == (3, 2, 16, 64) and not bool(c.k_pages.float().any() or c.v_pages.float().any())
+
+
+@pytest.mark.gpu
+def test_workspaces_of_a_growing_batch_stay_bounded():
+    hq, hkv, d = 2, 1, 64
+    caches = PagedCaches.allocate(200, 200, 16, hkv, d, 16)
+    for i in range(200):
+        caches.reserve(i, 16)
+    dec = PagedDecoder(caches, hq, 10000.0)
+    for k in range(1, 201):
+        q, kn, vn = new_rows(k, hq, hkv, d, k, False)
+        dec.step(torch.zeros(k, dtype=torch.int32, device="cuda"), q, kn, vn)
+    assert dec.device_status() == 0
+    sizes = [b for _, b in dec._workspaces]
+    assert sum(sizes) <= 2 * sizes[-1] and sizes[-1] <= 2 * pp.pp_paged_decode_workspace_bytes(dec.params, 200, 0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shared", [False, True])
+def test_nothing_is_read_from_a_workspace_that_was_not_written(shared):
+    """The same step over a workspace of zeros and over one whose numbers are all NaN, with rows of no prompt inside a group."""
+    hq, hkv, d, page = 8, 2, 128, 16
+    lengths = np.array([70, -1, 90, 64, 0, 130, -1, 300], np.int32)
+    caches = PagedCaches.allocate(len(lengths), 90, 330, hkv, d, page)
+    caches.reserve(0, 71)
+    for i in range(1, len(lengths)):
+        if i in (2, 3):
+            caches.share(0, i, 64)
+        if lengths[i] >= 0:
+            caches.reserve(i, int(lengths[i]) + 1)
+    caches.k_pages.normal_()
+    caches.v_pages.normal_()
+    ln = torch.from_numpy(lengths).cuda()
+    q, k, v = new_rows(len(lengths), hq, hkv, d, 5, False)
+    groups = (torch.tensor([0, 4, 6], dtype=torch.int32, device="cuda"), torch.tensor([64, 0], dtype=torch.int32, device="cuda")) if shared else None
+    dec = PagedDecoder(caches, hq, 10000.0)
+    outs = []
+    dec.step(ln, q, k, v, groups=groups)
+    for byte in (0, 255):
+        dec._workspaces[-1][0].fill_(byte)
+        out = torch.full((len(lengths), hq, d), 7.0, dtype=BF16, device="cuda")
+        outs.append(dec.step(ln, q, k, v, out=out, groups=groups).cpu())
+    assert dec.device_status() == 0 and torch.equal(*outs)
+    assert bool((outs[0][1] == 7).all() and (outs[0][6] == 7).all()) and bool(torch.isfinite(outs[0]).all())
+
+
+@pytest.mark.gpu
+def test_no_groups_is_the_step_without_them():
+    hq, hkv, d = 4, 2, 64
+    caches = PagedCaches.allocate(2, 8, 40, hkv, d, 16)
+    for i in range(2):
+        caches.reserve(i, 30)
+    caches.k_pages.normal_()
+    caches.v_pages.normal_()
+    ln = torch.tensor([20, 29], dtype=torch.int32, device="cuda")
+    q, _, _ = new_rows(2, hq, hkv, d, 9, False)
+    dec = PagedDecoder(caches, hq, 10000.0)
+    none = (torch.zeros(1, dtype=torch.int32, device="cuda"), torch.zeros(0, dtype=torch.int32, device="cuda"))
+    assert torch.equal(dec.step(ln, q), dec.step(ln, q, groups=none))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shared", [False, True])
+def test_step_of_the_most_prompts(shared):
+    """8192 prompts, and with shared rows 4096 groups of two: every row against the float64 form."""
+    hq, hkv, d, page, k = 2, 1, 64, 16, 8192
+    g = torch.Generator(device="cuda").manual_seed(3)
+    n_pages = k // 2 + k
+    caches = PagedCaches.allocate(1, n_pages, 16, hkv, d, page)
+    table = torch.empty((k, 2), dtype=torch.int32, device="cuda")
+    table[:, 0] = torch.arange(k, device="cuda", dtype=torch.int32) // 2
+    table[:, 1] = k // 2 + torch.arange(k, device="cuda", dtype=torch.int32)
+    pools = [torch.randn((n_pages, hkv, page, d), device="cuda", dtype=BF16, generator=g) for _ in range(2)]
+    caches = PagedCaches(*pools, table)
+    lengths = torch.randint(16, 33, (k,), dtype=torch.int32, device="cuda", generator=g)
+    q = torch.randn((k, hq, d), device="cuda", dtype=BF16, generator=g)
+    groups = (2 * torch.arange(k // 2 + 1, dtype=torch.int32, device="cuda"), torch.full((k // 2,), 16, dtype=torch.int32, device="cuda")) if shared else None
+    dec = PagedDecoder(caches, hq, 10000.0)
+    out = dec.step(lengths, q, groups=groups)
+    assert dec.device_status() == 0
+    rows = [x[table.long()][:, :, 0].reshape(k, 2 * page, d).double() for x in pools]
+    turned = torch.from_numpy(rotate64(host64(q), lengths.cpu().numpy() - 1, 10000.0)).cuda()
+    s = torch.einsum("khd,krd->khr", turned, rows[0]) / math.sqrt(d)
+    s = s.masked_fill(torch.arange(2 * page, device="cuda")[None, None, :] >= lengths[:, None, None], -math.inf)
+    p = torch.softmax(s, -1)
+    want = torch.einsum("khr,krd->khd", p, rows[1])
+    # O is rounded to bf16 once: 2^-8 of it. A query reaches the products as two bf16 numbers (2^-16 of it), over shared rows as one
+    # (2^-8); 2^-17 for the rotation and a sum of 64 products in fp32. That moves a score by at most e = (that) sum |q k| scale, and so
+    # a weight over the sum of them by a factor of exp(2 e) at most. A weight is one bf16 number over shared rows (2^-8 of it),
+    # else two, the first of them cut (2^-7 2^-8); 2^-17 for the sums over at most 33 rows in fp32. All of it times sum p |v|.
+    q_part, p_part = (2.0 ** -8, 2.0 ** -8) if shared else (2.0 ** -16, 2.0 ** -15)
+    e = torch.einsum("khd,krd->khr", turned.abs(), rows[0].abs()).amax(-1, keepdim=True) / math.sqrt(d) * (q_part + 2.0 ** -17)
+    err = torch.einsum("khr,krd->khd", p, rows[1].abs()) * (torch.exp(2 * e) - 1 + p_part + 2.0 ** -17) * (1 + p_part)
+    tol = want.abs() * 2.0 ** -8 + err * (1 + 2.0 ** -8)
+    assert bool(((out.double() - want).abs() <= tol).all())
