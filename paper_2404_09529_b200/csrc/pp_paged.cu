@@ -1030,17 +1030,21 @@ step_prepare_kernel(const __grid_constant__ PrepareArgs p) {
         }
         uint32_t* words = a.q + ((int64_t)i * a.n_q_heads + h) * (R::kParts * D / 2);
         const uint32_t high[4] = {R::high(x[0], x[1]), R::high(x[2], x[3]), R::high(y[0], y[1]), R::high(y[2], y[3])};
+        const uint32_t low[4] = {R::low(x[0], x[1], high[0]), R::low(x[2], x[3], high[1]), R::low(y[0], y[1], high[2]), R::low(y[2], y[3], high[3])};
 #pragma unroll
         for (int n = 0; n < 4; ++n) {
           const int e = j + (n & 1) * 2 + (n >> 1) * kHalf;
           uint32_t* word = words + R::word_thread(e) * (R::kParts * D / 8) + R::word_index(e);
           word[0] = high[n];
-          if constexpr (R::kParts == 2) word[D / 8] = n < 2 ? R::low(x[2 * n], x[2 * n + 1], high[n]) : R::low(y[2 * n - 4], y[2 * n - 3], high[n]);
+          if constexpr (R::kParts == 2) word[D / 8] = low[n];
         }
         if (plan.n_groups > 0) {
           __nv_bfloat16* row = plan.q_rot + (((int64_t)kvh * k + i) * a.group + h - kvh * a.group) * D + j;
           *reinterpret_cast<uint2*>(row) = make_uint2(high[0], high[1]);
           *reinterpret_cast<uint2*>(row + kHalf) = make_uint2(high[2], high[3]);
+          row += (int64_t)k * a.n_q_heads * D;
+          *reinterpret_cast<uint2*>(row) = make_uint2(low[0], low[1]);
+          *reinterpret_cast<uint2*>(row + kHalf) = make_uint2(low[2], low[3]);
         }
       } else {
         char* row = a.c.k_pages + to + (int64_t)kvh * a.c.head_stride + j * kSize;
@@ -1407,7 +1411,7 @@ PagedWorkspace paged_workspace(const pp_attn_params& p, int32_t k, int32_t n_gro
     L.units = take(sizeof(int64_t));
     L.groups = take((size_t)n_groups * sizeof(SharedGroup));
     L.prompts = take((size_t)k * sizeof(int2));
-    L.q_rot = take((size_t)k * p.n_q_heads * p.head_dim * sizeof(__nv_bfloat16));
+    L.q_rot = take(2 * (size_t)k * p.n_q_heads * p.head_dim * sizeof(__nv_bfloat16));
     const size_t rows = (size_t)kSms * kSharedTileRows + 2 * (size_t)k * p.n_q_heads;
     L.shared_ml = take(rows * sizeof(float2));
     L.shared_o = take(rows * p.head_dim * sizeof(float));

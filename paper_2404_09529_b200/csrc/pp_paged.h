@@ -61,7 +61,7 @@ struct PagedWorkspace {
   size_t units;                         // int64: units in all
   size_t groups;                        // SharedGroup [n_groups]
   size_t prompts;                       // int2 [k]: first row that the prompt reads on its own, its group (-1: none)
-  size_t q_rot;                         // bf16 [Hkv][k * group][D]
+  size_t q_rot;                         // bf16 [upper, lower part][Hkv][k * group][D]
   size_t shared_ml, shared_o;           // float2, float[D]: parts
   size_t items, row_ml, row_o;          // int2 [k][Hkv]; float2, float[D] [k][Hq]: of items that are not cut
   size_t total;

@@ -8,7 +8,11 @@
 // line of (row tile pair, key tile) units (pp_paged.h), so that CTAs finish together whatever the groups are like.
 //   warp 0       finds the pieces, TMA-loads the K / V tiles of 128 keys into one ring; a lane per page (and 64 columns)
 //   warp 1       issues tcgen05.mma: S_t = Q_t K^T into TMEM, O_t += P_t V with P_t read from TMEM, for the two row tiles t
-//   warps 2-3    TMA-load Q of tile 0 / 1
+//   warps 2-3    TMA-load Q of tile 0 / 1, as two bf16 numbers, which the products add up: one alone moves O by as much as its last
+//                rounding does (16 samples of a prompt of 2000 tokens, against 64 bits: 2.7e-3 of O with one, 2.1e-3 with two, 1.7e-3 is the
+//                last rounding; 21.5 and 22.0 us; 24 prompts of 8 samples 167 and 173; 64 prompts behind 32 700 rows, heads of 64, 52.4 and 52.9).
+//                More than 128 queries of heads of 128 have one: both parts of both tiles would leave the ring three stages of five (256
+//                prompts behind 8200 rows: 2.8e-3 and 2.3e-3, 112 and 123 us). P is one bf16 number: two would double the softmax's conversions and PV.
 //   warps 4-7    softmax of tile 0, a thread per row: no row is split between threads, so nothing is exchanged
 //   warps 8-11   the same for tile 1
 // A tile's softmax runs while the other tile's products do. An item of at most 128 rows has no second row tile: the two then take its
@@ -42,7 +46,12 @@ template <int D> struct SharedCfg {
   static constexpr int kQBytes = BM * D * 2, kTileBytes = BN * D * 2;
   static constexpr int kStages = D == 128 ? 5 : 10;
   static constexpr int kMiscBytes = 1024;
-  static constexpr int kSmemBytes = kMiscBytes + 1024 + 2 * kQBytes + kStages * kTileBytes;     // tiles on 1024-byte boundaries
+  // Room for Q: tile t's part x at (2 t + x) kQBytes, or, where there is only half of it, one part of either tile, or both of tile 0
+  // where tile 1 takes the same queries.
+  static constexpr int kQSlots = D == 128 ? 2 : 4;
+  static __device__ __forceinline__ uint32_t q_parts(bool split) { return kQSlots == 4 || split ? 2u : 1u; }
+  static __device__ __forceinline__ uint32_t q_at(uint32_t t, uint32_t part) { return ((kQSlots == 4 ? 2u : 1u) * t + part) * (uint32_t)kQBytes; }
+  static constexpr int kSmemBytes = kMiscBytes + 1024 + kQSlots * kQBytes + kStages * kTileBytes;     // tiles on 1024-byte boundaries
 };
 static_assert(SharedCfg<128>::kSmemBytes <= 227 * 1024 && SharedCfg<64>::kSmemBytes <= 227 * 1024, "shared memory");
 
@@ -67,7 +76,7 @@ __device__ __forceinline__ void load_page(uint32_t dst, const CUtensorMap* map, 
       ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(row), "r"(chunk), "r"(head), "r"(page), "r"(issue), "r"(0)
       : "memory");
 }
-// Coordinates: column (0), row, chunk (0), head.
+// Coordinates: column (0), row, chunk (0), head (those of the lower parts behind those of the upper ones).
 __device__ __forceinline__ void load_queries(uint32_t dst, const CUtensorMap* map, uint32_t bar, int row, int head, uint32_t issue) {
   asm volatile(
       "{\n.reg .pred q;\nsetp.ne.b32 q, %5, 0;\n"
@@ -86,7 +95,7 @@ shared_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   const uint32_t s_misc = smem_u32(smem_raw);
   const uint32_t s_q = (s_misc + Cfg::kMiscBytes + 1023u) & ~1023u;
-  const uint32_t s_kv = s_q + 2 * Cfg::kQBytes;
+  const uint32_t s_kv = s_q + Cfg::kQSlots * Cfg::kQBytes;
   const uint32_t bar_item_full = s_misc, bar_item_empty = s_misc + 32;      // [kRing] each
   const uint32_t bar_q_full = s_misc + 64, bar_q_empty = s_misc + 80;       // [2] each, and so on
   const uint32_t bar_s_full = s_misc + 96, bar_p_full = s_misc + 112;
@@ -227,14 +236,21 @@ shared_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
       auto issue_qk = [&](int t, int j) {
         const uint32_t s = (kv + 2u * (uint32_t)j) % NS;
         tc_fence_after();
-        const uint32_t a = q_lo + (split ? 0u : (uint32_t)t) * (Cfg::kQBytes >> 4), b = k_lo + s * (Cfg::kTileBytes >> 4);
+        const uint32_t b = k_lo + s * (Cfg::kTileBytes >> 4);
+#pragma unroll 1
+        for (uint32_t part = 0; part < Cfg::q_parts(split); ++part) {
+          const uint32_t a = q_lo + (Cfg::q_at(split ? 0u : (uint32_t)t, part) >> 4);
 #pragma unroll
-        for (int kk = 0; kk < D / 16; ++kk)
-          mma_ss(tmem_base + 128u * t, a + (uint32_t)(kk >> 2) * ((BM * 128) >> 4) + (uint32_t)(kk & 3) * 2,
-                 b + (uint32_t)(kk >> 2) * ((BN * 128) >> 4) + (uint32_t)(kk & 3) * 2, idesc_qk, kk > 0 ? 1u : 0u, issue);
+          for (int kk = 0; kk < D / 16; ++kk)
+            mma_ss(tmem_base + 128u * t, a + (uint32_t)(kk >> 2) * ((BM * 128) >> 4) + (uint32_t)(kk & 3) * 2,
+                   b + (uint32_t)(kk >> 2) * ((BN * 128) >> 4) + (uint32_t)(kk & 3) * 2, idesc_qk, kk > 0 || part > 0 ? 1u : 0u, issue);
+        }
         tc_commit(bar_s_full + 8 * t, issue);
         if (t == 1 || split) tc_commit(bar_kv_empty + 8 * s, issue);
-        if (j + 1 == n) tc_commit(bar_q_empty + (split ? 0 : 8 * t), issue);
+        if (j + 1 == n) {
+          tc_commit(bar_q_empty + (split ? 0 : 8 * t), issue);
+          if (split) tc_commit(bar_q_empty + 8, issue);       // (tile 1's room for queries may hold tile 0's lower part)
+        }
       };
       // O_t (+)= P_t V_j, then the tile's next scores, those of key tile `next`. The next K is waited for first where it has been there
       // for long (both row tiles read it); of an item that is split it may be the one that is loaded last.
@@ -290,7 +306,6 @@ shared_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
             if (!(ok = mbar_wait_issuer<kWaitOEmpty>(bar_o_empty + 8, (it_n & 1u) ^ 1u, wctx))) break;
             if (issue) mbar_arrive(bar_o_full + 8);
           }
-          if (ok && issue) mbar_arrive(bar_q_empty + 8);       // (no query was loaded for it)
         }
         if (!ok) break;
         kv += 2u * (uint32_t)n;
@@ -309,8 +324,12 @@ shared_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
         if (n < 0) break;
         if (!mbar_wait_issuer<kWaitQEmpty>(bar_q_empty + 8 * t, (it_n & 1u) ^ 1u, wctx)) break;
         if (t == 0 || rows > BM) {
-          mbar_expect_tx(bar_q_full + 8 * t, Cfg::kQBytes, issue);
-          load_queries(s_q + t * Cfg::kQBytes, &map_q, bar_q_full + 8 * t, q_row + BM * t, kv_head, issue);
+          // (the lower part may go where tile 1's queries of the item before were)
+          const uint32_t parts = Cfg::q_parts(rows <= BM);
+          if (Cfg::kQSlots == 2 && parts == 2 && !mbar_wait_issuer<kWaitQEmpty>(bar_q_empty + 8, (it_n & 1u) ^ 1u, wctx)) break;
+          mbar_expect_tx(bar_q_full + 8 * t, parts * Cfg::kQBytes, issue);
+          for (uint32_t part = 0; part < parts; ++part)
+            load_queries(s_q + Cfg::q_at((uint32_t)t, part), &map_q, bar_q_full + 8 * t, q_row + BM * t, (int)part * args.n_kv_heads + kv_head, issue);
         } else if (issue) {
           mbar_arrive(bar_q_full + 8 * t);
         }
@@ -448,7 +467,7 @@ int launch(const pp_attn_params& p, const PagedCacheArgs& c, const SharedArgs& a
   using Cfg = SharedCfg<D>;
   CUtensorMap mq, mk, mv;
   const cuuint64_t q_rows = (cuuint64_t)k * (cuuint64_t)a.group;
-  const cuuint64_t q_dims[4] = {64u, q_rows, D / 64, (cuuint64_t)p.n_kv_heads}, q_strides[3] = {D * 2, 128u, q_rows * D * 2};
+  const cuuint64_t q_dims[4] = {64u, q_rows, D / 64, 2 * (cuuint64_t)p.n_kv_heads}, q_strides[3] = {D * 2, 128u, q_rows * D * 2};
   const cuuint32_t q_box[4] = {64u, BM, D / 64, 1u};
   const cuuint64_t page_rows = (cuuint64_t)1 << c.page_shift;
   const cuuint64_t dims[5] = {64u, page_rows, D / 64, (cuuint64_t)p.n_kv_heads, (cuuint64_t)c.n_pages};
