@@ -9,10 +9,11 @@
 //   warp 0       finds the pieces, TMA-loads the K / V tiles of 128 keys into one ring; a lane per page (and 64 columns)
 //   warp 1       issues tcgen05.mma: S_t = Q_t K^T into TMEM, O_t += P_t V with P_t read from TMEM, for the two row tiles t
 //   warps 2-3    TMA-load Q of tile 0 / 1, as two bf16 numbers, which the products add up: one alone moves O by as much as its last
-//                rounding does (16 samples of a prompt of 2000 tokens, against 64 bits: 2.7e-3 of O with one, 2.1e-3 with two, 1.7e-3 is the
-//                last rounding; 21.5 and 22.0 us; 24 prompts of 8 samples 167 and 173; 64 prompts behind 32 700 rows, heads of 64, 52.4 and 52.9).
-//                More than 128 queries of heads of 128 have one: both parts of both tiles would leave the ring three stages of five (256
-//                prompts behind 8200 rows: 2.8e-3 and 2.3e-3, 112 and 123 us). P is one bf16 number: two would double the softmax's conversions and PV.
+//                rounding does (against 64 bits, O's last rounding being 1.7e-3 of it: 16 samples of a prompt of 2000 rows 2.7e-3 with
+//                one, 2.1e-3 with two, 22.0 and 22.4 us; 24 prompts of 8 samples 2.6e-3 and 2.1e-3, 178 and 193; 64 prompts behind 32 700
+//                rows, heads of 64, 2.9e-3 and 2.3e-3, 52.4 and 52.9). More than 128 queries of heads of 128 have one: both parts of both
+//                tiles would leave the ring three stages of five (256 prompts behind 8200 rows: 2.8e-3 and 2.3e-3, 112 and 123 us).
+//                P is one bf16 number: two would double the conversions of the softmax, which bounds, and P V.
 //   warps 4-7    softmax of tile 0, a thread per row: no row is split between threads, so nothing is exchanged
 //   warps 8-11   the same for tile 1
 // A tile's softmax runs while the other tile's products do. An item of at most 128 rows has no second row tile: the two then take its
