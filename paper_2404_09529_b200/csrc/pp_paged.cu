@@ -50,10 +50,10 @@ __device__ __forceinline__ uint32_t round_e4m3(float a, float b, float c, float 
 // ------------------------------------------------------------------------------------------
 // Rows into pages
 // ------------------------------------------------------------------------------------------
-// A copy with a rotation in it, bound by HBM: a CTA takes as many rows (or heads of one) as make 2048 elements of K. A thread has one pair of 8-element
-// pieces of K (c and D/2 + c) and two pieces of V of the same row, so that all it needs is that row's prompt and position:
-// its loads, the page's number and the angles (once for all heads of a row, through shared memory) are then under way together.
-// 17 554 rows of 32 heads of 128 take 89 us (6.5 TB/s; 114 with the row's place found first and handed round), 44 k short rows of
+// A copy with a rotation in it, bound by HBM: a CTA takes as many rows (or heads of one) as make 2048 elements of K. A thread has one
+// pair of 8-element pieces of K (c and D/2 + c) and two pieces of V of the same row, so that all it needs is that row's prompt and
+// position: its loads, the page's number and the angles (once for all heads of a row, through shared memory) are then under way together.
+// 17 554 rows of 32 heads of 128 take 89 to 92 us (6.3 TB/s and more; 114 with the row's place found first and handed round), 44 k short rows of
 // 8 heads of 64 into 8 bits 33 us (4.1 TB/s, was 55), where instructions count: 430 a thread, a quarter of them for the angle, and as
 // many for the conversions.
 constexpr int kAppendThreads = 128;
@@ -197,9 +197,9 @@ append_kernel(const __grid_constant__ AppendArgs a) {
 // two units in shared memory, whose loads run ahead over the ends of items. Six warps (seven over 8-bit pages, which take more
 // instructions a byte) keep up to 96 KB of an SM under way, which is all that HBM takes: with twelve, the loads queued up and SMs
 // were served so unevenly that of 148 equal shares the last ended 20 % after the mean. A piece that is a whole item (prompt, KV head)
-// leaves O at once. What an item costs beside its rows is the latency of one warp: with the queries rotated there, and the new token a step
-// of its own, 4700 cycles of 1800 a unit (prepared apart: 64 prompts on 32 heads 57.8 -> 56.9 us,
-// 64 prompts behind one document of 4096 rows 59 -> 55, 16 samples of one prompt 25.9 -> 23.7; ten prompts on one layer 11.4 -> 12.1).
+// leaves O at once. What an item costs beside its rows is the latency of one warp: with the queries rotated there, and the new token a
+// step of its own, 4700 cycles, a unit 1800 (prepared apart: 64 prompts on 32 heads 57.8 -> 56.9 us, 64 prompts behind one document
+// of 32 700 rows 59 -> 55, 16 samples of one prompt 25.9 -> 23.7; ten prompts on one layer 11.4 -> 12.1).
 // The arithmetic is that of the step over contiguous caches (pp_decode.cu): mma.m16n8k16 with 16 keys as rows and the query heads
 // of a KV head as the 8 columns, absent heads 0. Over bf16 pages a query and a weight each reach it as the sum of two
 // 16-bit numbers: HBM leaves the tensor cores idle, and scores and O are then exact to 2^-16, far below O's last rounding of 2^-8.
