@@ -986,3 +986,76 @@ def test_step_of_the_most_prompts(shared):
     err = torch.einsum("khr,krd->khd", p, rows[1].abs()) * (torch.exp(2 * e) - 1 + p_part + 2.0 ** -17) * (1 + p_part)
     tol = want.abs() * 2.0 ** -8 + err * (1 + 2.0 ** -8)
     assert bool(((out.double() - want).abs() <= tol).all())
+
+
+def _random_caches(lengths, room, hkv, d, page, shared_pages=0):
+    """Caches of random contents whose prompts begin with the same pages."""
+    n = len(lengths)
+    caches = PagedCaches.allocate(n, n * -(-room // page), room, hkv, d, page)
+    caches.reserve(0, room)
+    for i in range(1, n):
+        caches.share(0, i, shared_pages * page)
+        caches.reserve(i, room)
+    caches.k_pages.normal_()
+    caches.v_pages.normal_()
+    return caches
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shared", [False, True])
+def test_steps_queued_one_behind_the_other_are_the_steps_alone(shared):
+    """Kernels of neighbouring calls overlap; what each of them reads must be there all the same. Appends, steps and changes of the
+    lengths, queued without a pause, against the same calls with a synchronisation after each."""
+    hq, hkv, d, page, n, steps = 8, 2, 128, 16, 12, 40
+    lengths = np.arange(n, dtype=np.int32) * 37 + 70
+    groups = (torch.tensor([0, 8, n], dtype=torch.int32, device="cuda"), torch.tensor([64, 48], dtype=torch.int32, device="cuda")) if shared else None
+    torch.manual_seed(11)
+    first = _random_caches(lengths, 600, hkv, d, page, 4)
+    state = first.k_pages.clone(), first.v_pages.clone()
+    new = [new_rows(n, hq, hkv, d, 100 + s, False) for s in range(steps)]
+    extra = [new_rows(n, hq, hkv, d, 200 + s, False) for s in range(steps)]
+    every = torch.arange(n, dtype=torch.int32, device="cuda")
+
+    def run(pause):
+        first.k_pages.copy_(state[0])
+        first.v_pages.copy_(state[1])
+        dec, ln, outs = PagedDecoder(first, hq, 10000.0), torch.from_numpy(lengths).cuda(), []
+        torch.cuda.synchronize()
+        for s in range(steps):
+            q, k, v = new[s]
+            outs.append(dec.step(ln, q, k, v, groups=groups))
+            if pause:
+                torch.cuda.synchronize()
+            ln += 1
+            if s % 3 == 0:                             # a row more, by the other call
+                first.append(every, ln, extra[s][1], extra[s][2], 10000.0)
+                ln += 1
+            if pause:
+                torch.cuda.synchronize()
+        torch.cuda.synchronize()
+        assert dec.device_status() == 0 and int(first.status) == 0
+        return torch.stack(outs), first.k_pages.clone(), first.v_pages.clone()
+
+    for a, b in zip(run(True), run(False)):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.gpu
+def test_steps_on_two_streams_at_once():
+    hq, hkv, d, page, n = 8, 2, 64, 32, 20
+    lengths = np.arange(n, dtype=np.int32) * 53 + 130
+    torch.manual_seed(12)
+    caches = _random_caches(lengths, 1200, hkv, d, page, 4)
+    ln = torch.from_numpy(lengths).cuda()
+    groups = (torch.tensor([0, n], dtype=torch.int32, device="cuda"), torch.tensor([128], dtype=torch.int32, device="cuda"))
+    qs = [new_rows(n, hq, hkv, d, 300 + s, False)[0] for s in range(2)]
+    want = [PagedDecoder(caches, hq, 10000.0).step(ln, qs[0]), PagedDecoder(caches, hq, 10000.0).step(ln, qs[1], groups=groups)]
+    torch.cuda.synchronize()
+    streams, decs = [torch.cuda.Stream() for _ in range(2)], [PagedDecoder(caches, hq, 10000.0) for _ in range(2)]
+    outs = [[], []]
+    for _ in range(30):
+        for x in range(2):
+            with torch.cuda.stream(streams[x]):
+                outs[x].append(decs[x].step(ln, qs[x], groups=groups if x else None))
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want[x]) for x in range(2) for o in outs[x]) and decs[0].device_status() == decs[1].device_status() == 0
