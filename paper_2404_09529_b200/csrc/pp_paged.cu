@@ -7,6 +7,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 
 #include "pp_decode_tile.h"
@@ -1026,7 +1027,12 @@ step_prepare_kernel(const __grid_constant__ PrepareArgs p) {
           const float down = __uint_as_float((uint32_t)(127 - shift) << 23);
 #pragma unroll
           for (int e = 0; e < 4; ++e) { x[e] *= down; y[e] *= down; }
-          if (j == 0) a.q_factor[(int64_t)i * a.n_q_heads + h] = a.scale_log2 * a.c.k_scale[kvh] * __uint_as_float((uint32_t)(127 + shift) << 23);
+          // The factor stays a normal number: hidden rows are -inf before it is applied, and -inf times 0 would be a NaN. (A query of zeros
+          // over keys of a scale below 7e-9 had a factor of 0. One of 2^-126 brings every sum of products to below 2^-109 too.)
+          if (j == 0) {
+            const double factor = (double)a.scale_log2 * a.c.k_scale[kvh] * __uint_as_float((uint32_t)(127 + shift) << 23);
+            a.q_factor[(int64_t)i * a.n_q_heads + h] = (float)fmin(fmax(factor, (double)FLT_MIN), (double)FLT_MAX);
+          }
         }
         uint32_t* words = a.q + ((int64_t)i * a.n_q_heads + h) * (R::kParts * D / 2);
         const uint32_t high[4] = {R::high(x[0], x[1]), R::high(x[2], x[3]), R::high(y[0], y[1]), R::high(y[2], y[3])};
