@@ -296,7 +296,7 @@ int pp_decode_step(const pp_attn_params* params, const int32_t* lengths, int32_t
  *                      [page, head, row, D] and [page, row, head, D] alike. Strides are multiples of 16 bytes, at least D, and
  *                      no two rows may overlap.
  *   k_scale, v_scale   device float [Hkv], for PP_CACHE_E4M3 (NULL otherwise): a stored number stands for itself times
- *                      the scale of its KV head. Finite, above 0.
+ *                      the scale of its KV head. Normal numbers above 0 (2^-126 and more, so that the reciprocal is finite).
  *   page_table         device int32 [k, table_stride]. Entries of rows that a prompt does not have are not used, whatever they hold.
  *   n_pages            pages of either pool. An entry outside 0 .. n_pages - 1 where a row is needed is not followed:
  *                      the call sets the status word (PP_PAGED_*) and that prompt's results are unspecified.

@@ -395,7 +395,7 @@ struct Rows<D, false> {
     return 16 * (r >> 1) + 8 * (r & 1) + g;
   }
   // O of the eight heads as rows of bf16, heads 2t and 2t + 1 times f0 and f1 (transposed, a lane holds pairs of elements of one head)
-  static __device__ __forceinline__ void leave(const float (&acc)[D / 16][4], float f0, float f1, uint32_t at, int g, int t) {
+  static __device__ __forceinline__ void leave(const float (&acc)[D / 16][4], float f0, float f1, float, uint32_t at, int g, int t) {
 #pragma unroll
     for (int j = 0; j < D / 16; ++j)
 #pragma unroll
@@ -493,12 +493,12 @@ struct Rows<D, true> {
   }
   static __device__ __forceinline__ int element(int j, int x, int g) { return (D / 8) * g + 2 * j + x; }
   static __device__ __forceinline__ int element_at(int place) { return place; }
-  static __device__ __forceinline__ void leave(const float (&acc)[D / 16][4], float f0, float f1, uint32_t at, int g, int t) {
+  static __device__ __forceinline__ void leave(const float (&acc)[D / 16][4], float f0, float f1, float v_scale, uint32_t at, int g, int t) {
 #pragma unroll
     for (int j = 0; j < D / 16; ++j)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const uint32_t w = round_bf16(acc[j][h] * (h ? f1 : f0), acc[j][2 + h] * (h ? f1 : f0));
+        const uint32_t w = round_bf16(acc[j][h] * (h ? f1 : f0) * v_scale, acc[j][2 + h] * (h ? f1 : f0) * v_scale);
         asm volatile("st.shared.u32 [%0], %1;" ::"r"(at + 2 * ((2 * t + h) * D + (D / 8) * g + 2 * j)), "r"(w) : "memory");
       }
   }
@@ -791,7 +791,9 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
       phase ^= stage ^ 1;               // (after every second unit)
     }
     // ---- out
-    const float out_scale = (kE4m3 ? a.c.v_scale[c.kvh] : 1.f) / R::kWeight;
+    // (Products with the scale of the values come last: divided by a sum of weights it may have no bits left in fp32.)
+    const float v_scale = kE4m3 ? a.c.v_scale[c.kvh] : 1.f;
+    auto part = [&](float x) { return kE4m3 ? x * (1.f / R::kWeight) * v_scale : x; };
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -799,7 +801,7 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
     if (begins && ends && !a.items) {
       // (a row that attends to nothing is 0; one all of whose scores are -inf is a NaN)
       const bool none = c.len == 0;
-      R::leave(acc, none ? 0.f : out_scale / l[0], none ? 0.f : out_scale / l[1], scratch, g, t);
+      R::leave(acc, none ? 0.f : 1.f / (l[0] * R::kWeight), none ? 0.f : 1.f / (l[1] * R::kWeight), v_scale, scratch, g, t);
       __syncwarp();
       __nv_bfloat16* to = a.o + ((int64_t)c.i * a.n_q_heads + c.kvh * a.group) * D;
       for (int x = lane; x < a.group * D / 8; x += 32) *reinterpret_cast<uint4*>(to + 8 * x) = shared16(scratch + 16 * x);
@@ -818,9 +820,8 @@ paged_decode_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_cons
 #pragma unroll
         for (int j = 0; j < D / 16; j += 4)       // (whole sectors: 32 bytes a store)
           asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
-                       ::"l"(to + 2 * j), "f"(acc[j][h] * out_scale), "f"(acc[j][2 + h] * out_scale), "f"(acc[j + 1][h] * out_scale),
-                         "f"(acc[j + 1][2 + h] * out_scale), "f"(acc[j + 2][h] * out_scale), "f"(acc[j + 2][2 + h] * out_scale),
-                         "f"(acc[j + 3][h] * out_scale), "f"(acc[j + 3][2 + h] * out_scale) : "memory");
+                       ::"l"(to + 2 * j), "f"(part(acc[j][h])), "f"(part(acc[j][2 + h])), "f"(part(acc[j + 1][h])), "f"(part(acc[j + 1][2 + h])),
+                         "f"(part(acc[j + 2][h])), "f"(part(acc[j + 2][2 + h])), "f"(part(acc[j + 3][h])), "f"(part(acc[j + 3][2 + h])) : "memory");
       }
       if (begins && lane == 0) {        // the pieces over which the item goes on: units behind this one's end
         const int parts = whole ? 0 : 1 + (int)((c.units - c.n + per - 1) / per);
