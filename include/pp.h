@@ -390,8 +390,8 @@ int pp_paged_decode_step(const pp_attn_params* params, const pp_paged_cache* cac
  *   cache        PP_CACHE_BF16 only
  *   workspace    >= pp_paged_decode_workspace_bytes(params, k, n_groups)
  * The shared rows must hold finite values (a value that is not makes every query of the group that reads it NaN or infinite
- * in that element, whatever its weight). Their probabilities are rounded to bf16 as in the prefill; so are the rotated queries that
- * meet them where head_dim is 128 and a group has more than 128 of them for a KV head (else: two bf16 numbers, 2^-16).
+ * in that element, whatever its weight). Their probabilities are rounded to bf16 as in the prefill; the rotated queries that meet them
+ * are two bf16 numbers each (2^-16).
  * device_status also reports a wait that gave up, as in pp_prefill_attention. Errors as pp_paged_decode_step; PP_ERR_UNSUPPORTED
  * for an 8-bit cache.
  */

@@ -1083,10 +1083,10 @@ step_prepare_kernel(const __grid_constant__ PrepareArgs p) {
   if (blockIdx.y > 0) return;
   extern __shared__ int32_t s_plan[];   // group_ptr [n_groups + 1], the rows shared [n_groups], the first prompt of each group
   __shared__ int64_t s_warp[kPrepareThreads / 32];
-  __shared__ int s_bad;
+  __shared__ int s_bad, s_wide;
   const int n = plan.n_groups;
   int32_t *s_ptr = s_plan, *s_rows = s_plan + n + 1, *s_lead = s_rows + n;
-  if (tid == 0) s_bad = 0;
+  if (tid == 0) s_bad = s_wide = 0;
   __syncthreads();
   for (int g = tid; g <= n; g += kPrepareThreads) {
     const int at = plan.group_ptr[g], before = g ? plan.group_ptr[g - 1] : 0;
@@ -1124,6 +1124,7 @@ step_prepare_kernel(const __grid_constant__ PrepareArgs p) {
     const int prompts = bad ? 0 : s_ptr[g + 1] - s_ptr[g];
     const int rows = prompts > 0 && s_lead[g] < k ? s_rows[g] & ~page_mask : 0;      // (a group may be all rows of no prompt)
     s_rows[g] = rows;
+    if (rows > 0 && prompts * a.group > kSharedTileRows / 2) s_wide = 1;
     const int tiles = (rows + kSharedTileKeys - 1) / kSharedTileKeys;
     units += (int64_t)tiles * ((prompts * a.group + kSharedTileRows - 1) / kSharedTileRows) * a.n_kv_heads;
     parts += (int64_t)shared_part_rows(prompts * a.group) * a.n_kv_heads;
@@ -1143,7 +1144,10 @@ step_prepare_kernel(const __grid_constant__ PrepareArgs p) {
     at += (int64_t)x.key_tiles * ((x.query_rows + kSharedTileRows - 1) / kSharedTileRows) * a.n_kv_heads;
     part += (int64_t)shared_part_rows(x.query_rows) * a.n_kv_heads;
   }
-  if (tid == 0) *plan.units = all;
+  if (tid == 0) {
+    plan.units[0] = all;
+    plan.units[1] = s_wide;
+  }
   __syncthreads();
   for (int i = tid; i < k; i += kPrepareThreads) {
     const int g = group_of(i);
@@ -1415,7 +1419,7 @@ PagedWorkspace paged_workspace(const pp_attn_params& p, int32_t k, int32_t n_gro
   L.part_ml = take(parts * sizeof(float2));
   L.part_o = take(parts * p.head_dim * sizeof(float));
   if (n_groups > 0) {
-    L.units = take(sizeof(int64_t));
+    L.units = take(2 * sizeof(int64_t));
     L.groups = take((size_t)n_groups * sizeof(SharedGroup));
     L.prompts = take((size_t)k * sizeof(int2));
     L.q_rot = take(2 * (size_t)k * p.n_q_heads * p.head_dim * sizeof(__nv_bfloat16));

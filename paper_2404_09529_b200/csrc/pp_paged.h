@@ -58,7 +58,7 @@ struct PagedWorkspace {
   size_t q, q_factor;                   // the queries as the products take them
   size_t part_ml, part_o;               // float2, float[D]
   // with shared rows only
-  size_t units;                         // int64: units in all
+  size_t units;                         // int64 [2]: units in all; whether some group has more than half a row tile of queries
   size_t groups;                        // SharedGroup [n_groups]
   size_t prompts;                       // int2 [k]: first row that the prompt reads on its own, its group (-1: none)
   size_t q_rot;                         // bf16 [upper, lower part][Hkv][k * group][D]

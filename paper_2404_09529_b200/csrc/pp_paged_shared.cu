@@ -10,9 +10,8 @@
 //   warp 1       issues tcgen05.mma: S_t = Q_t K^T into TMEM, O_t += P_t V with P_t read from TMEM, for the two row tiles t
 //   warps 2-3    TMA-load Q of tile 0 / 1, as two bf16 numbers, which the products add up: one alone moves O by as much as its last
 //                rounding does (against 64 bits, O's last rounding being 1.7e-3 of it: 16 samples of a prompt of 2000 rows 2.7e-3 with
-//                one, 2.1e-3 with two, 22.0 and 22.4 us; 24 prompts of 8 samples 2.6e-3 and 2.1e-3, 178 and 193; 64 prompts behind 32 700
-//                rows, heads of 64, 2.9e-3 and 2.3e-3, 52.4 and 52.9). More than 128 queries of heads of 128 have one: both parts of both
-//                tiles would leave the ring three stages of five (256 prompts behind 8200 rows: 2.8e-3 and 2.3e-3, 112 and 123 us).
+//                one, 2.1e-3 with two, 22.0 and 22.3 us; 24 prompts of 8 samples 2.6e-3 and 2.1e-3, 178 and 190; 64 prompts behind 32 700
+//                rows, heads of 64, 2.9e-3 and 2.3e-3, 52.4 and 52.8; 256 prompts behind 8200 rows 2.9e-3 and 2.3e-3, 112 and 119).
 //                P is one bf16 number: two would double the conversions of the softmax, which bounds, and P V.
 //   warps 4-7    softmax of tile 0, a thread per row: no row is split between threads, so nothing is exchanged
 //   warps 8-11   the same for tile 1
@@ -45,14 +44,17 @@ constexpr float kLazyLog2 = 8.f;
 
 template <int D> struct SharedCfg {
   static constexpr int kQBytes = BM * D * 2, kTileBytes = BN * D * 2;
-  static constexpr int kStages = D == 128 ? 5 : 10;
   static constexpr int kMiscBytes = 1024;
-  // Room for Q: tile t's part x at (2 t + x) kQBytes, or, where there is only half of it, one part of either tile, or both of tile 0
-  // where tile 1 takes the same queries.
-  static constexpr int kQSlots = D == 128 ? 2 : 4;
-  static __device__ __forceinline__ uint32_t q_parts(bool split) { return kQSlots == 4 || split ? 2u : 1u; }
-  static __device__ __forceinline__ uint32_t q_at(uint32_t t, uint32_t part) { return ((kQSlots == 4 ? 2u : 1u) * t + part) * (uint32_t)kQBytes; }
-  static constexpr int kSmemBytes = kMiscBytes + 1024 + kQSlots * kQBytes + kStages * kTileBytes;     // tiles on 1024-byte boundaries
+  // Tile t's part x of Q lies at (2 t + x) kQBytes, and behind the queries the ring. Both parts of both tiles leave it three stages with
+  // heads of 128. Where no group has more than 128 queries for a KV head, nothing needs the second tile's room, and it has five (24 prompts
+  // of 8 samples, 32 heads of 128: 190 us with five, 204 with three).
+  static constexpr int kSlots = D == 128 ? 7 : 14;
+  static constexpr int kStages = D == 128 ? 5 : 10, kWideStages = D == 128 ? 3 : 10;
+  static __device__ __forceinline__ uint32_t q_at(uint32_t t, uint32_t part) { return (2u * t + part) * (uint32_t)kQBytes; }
+  static __device__ __forceinline__ uint32_t stage_of(uint32_t tile, bool wide) { return kStages == kWideStages || !wide ? tile % kStages : tile % kWideStages; }
+  static __device__ __forceinline__ uint32_t turn_of(uint32_t tile, bool wide) { return kStages == kWideStages || !wide ? tile / kStages : tile / kWideStages; }
+  static constexpr int kSmemBytes = kMiscBytes + 1024 + kSlots * kTileBytes;     // tiles on 1024-byte boundaries
+  static_assert(kQBytes == kTileBytes && 4 + kWideStages <= kSlots && (D == 64 ? 4 : 2) + kStages <= kSlots, "shared memory");
 };
 static_assert(SharedCfg<128>::kSmemBytes <= 227 * 1024 && SharedCfg<64>::kSmemBytes <= 227 * 1024, "shared memory");
 
@@ -96,7 +98,6 @@ shared_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   const uint32_t s_misc = smem_u32(smem_raw);
   const uint32_t s_q = (s_misc + Cfg::kMiscBytes + 1023u) & ~1023u;
-  const uint32_t s_kv = s_q + Cfg::kQSlots * Cfg::kQBytes;
   const uint32_t bar_item_full = s_misc, bar_item_empty = s_misc + 32;      // [kRing] each
   const uint32_t bar_q_full = s_misc + 64, bar_q_empty = s_misc + 80;       // [2] each, and so on
   const uint32_t bar_s_full = s_misc + 96, bar_p_full = s_misc + 112;
@@ -141,6 +142,9 @@ shared_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
   const uint32_t tmem_base = (uint32_t)uniform((int)*s_tmem_base);
   pdl_wait();                           // the plan, the rotated queries and the pages
   pdl_launch_dependents();
+  // of the whole launch: some group has more than 128 queries for a KV head
+  const bool wide = warp < 4 && args.plan.units[1] != 0;
+  const uint32_t s_kv = s_q + (D == 64 || wide ? 4u : 2u) * Cfg::kQBytes;
 
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
@@ -216,7 +220,7 @@ shared_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
             mbar_expect_tx(full, Cfg::kTileBytes, issue);
             __syncwarp();
             load_page(s_kv + stage * Cfg::kTileBytes + lane_dst, part ? &map_v : &map_k, full, row, chunk, kv_head, page, lane_issue);
-            if (++stage == NS) { stage = 0; phase ^= 1u; }
+            if (++stage == (wide ? (uint32_t)Cfg::kWideStages : NS)) { stage = 0; phase ^= 1u; }
           }
           page = page_next;
         }
@@ -232,14 +236,14 @@ shared_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
       uint32_t it_n = 0, kv = 0, count[2] = {0, 0};       // kv: K and V tiles of the items before (K of tile j: kv + 2j)
       int n = 0;
       bool split = false, ok = true;
-      auto wait_kv = [&](uint32_t at) { return mbar_wait_issuer<kWaitKvFull>(bar_kv_full + 8 * (at % NS), (at / NS) & 1u, wctx); };
+      auto wait_kv = [&](uint32_t at) { return mbar_wait_issuer<kWaitKvFull>(bar_kv_full + 8 * Cfg::stage_of(at, wide), Cfg::turn_of(at, wide) & 1u, wctx); };
       // The scores are what a tile's softmax waits for: their commit comes first, the one that gives the stages back after it.
       auto issue_qk = [&](int t, int j) {
-        const uint32_t s = (kv + 2u * (uint32_t)j) % NS;
+        const uint32_t s = Cfg::stage_of(kv + 2u * (uint32_t)j, wide);
         tc_fence_after();
         const uint32_t b = k_lo + s * (Cfg::kTileBytes >> 4);
 #pragma unroll 1
-        for (uint32_t part = 0; part < Cfg::q_parts(split); ++part) {
+        for (uint32_t part = 0; part < 2; ++part) {
           const uint32_t a = q_lo + (Cfg::q_at(split ? 0u : (uint32_t)t, part) >> 4);
 #pragma unroll
           for (int kk = 0; kk < D / 16; ++kk)
@@ -250,16 +254,17 @@ shared_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
         if (t == 1 || split) tc_commit(bar_kv_empty + 8 * s, issue);
         if (j + 1 == n) {
           tc_commit(bar_q_empty + (split ? 0 : 8 * t), issue);
-          if (split) tc_commit(bar_q_empty + 8, issue);       // (tile 1's room for queries may hold tile 0's lower part)
+          if (split) tc_commit(bar_q_empty + 8, issue);       // (a phase for each item, also where tile 1 has no queries of its own)
         }
       };
       // O_t (+)= P_t V_j, then the tile's next scores, those of key tile `next`. The next K is waited for first where it has been there
-      // for long (both row tiles read it); of an item that is split it may be the one that is loaded last.
+      // for long (heads of 64, unless the item is split). Otherwise it may be the one that is loaded last: the product goes first, and
+      // so does what gives V's stage back (256 prompts behind 8200 rows, heads of 128: 124.7 -> 118.7 us).
       auto step = [&](int t, int j, bool first, int next) -> bool {
         if (first && !mbar_wait_issuer<kWaitOEmpty>(bar_o_empty + 8 * t, (it_n & 1u) ^ 1u, wctx)) return false;
-        const uint32_t vc = kv + 2u * (uint32_t)j + 1u, s = vc % NS, kc = kv + 2u * (uint32_t)next;
+        const uint32_t vc = kv + 2u * (uint32_t)j + 1u, s = Cfg::stage_of(vc, wide), kc = kv + 2u * (uint32_t)next;
         if (!wait_kv(vc)) return false;
-        if (!split && next < n && !wait_kv(kc)) return false;
+        if (D == 64 && !split && next < n && !wait_kv(kc)) return false;
         if (!mbar_wait_issuer<kWaitP>(bar_p_full + 8 * t, count[t] & 1u, wctx)) return false;
         tc_fence_after();
         const uint32_t d = tmem_base + 256u + (uint32_t)(D * t), a = tmem_base + 128u * t, b = v_lo + s * (Cfg::kTileBytes >> 4);
@@ -268,12 +273,10 @@ shared_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
           mma_ts(d, a + kk * 8, b + (uint32_t)kk * ((16 * 128) >> 4), idesc_pv, kk > 0 || !first ? 1u : 0u, issue);
         ++count[t];
         if (next < n) {
-          if (split) {
-            tc_commit(bar_kv_empty + 8 * s, issue);
-            if (!wait_kv(kc)) return false;
-          }
+          if (split || (D == 128 && t == 1)) tc_commit(bar_kv_empty + 8 * s, issue);
+          if ((D == 128 || split) && !wait_kv(kc)) return false;
           issue_qk(t, next);
-          if (!split && t == 1) tc_commit(bar_kv_empty + 8 * s, issue);
+          if (D == 64 && !split && t == 1) tc_commit(bar_kv_empty + 8 * s, issue);
         } else {
           if (t == 1 || split) tc_commit(bar_kv_empty + 8 * s, issue);
           tc_commit(bar_o_full + 8 * t, issue);
@@ -325,11 +328,8 @@ shared_attention_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_
         if (n < 0) break;
         if (!mbar_wait_issuer<kWaitQEmpty>(bar_q_empty + 8 * t, (it_n & 1u) ^ 1u, wctx)) break;
         if (t == 0 || rows > BM) {
-          // (the lower part may go where tile 1's queries of the item before were)
-          const uint32_t parts = Cfg::q_parts(rows <= BM);
-          if (Cfg::kQSlots == 2 && parts == 2 && !mbar_wait_issuer<kWaitQEmpty>(bar_q_empty + 8, (it_n & 1u) ^ 1u, wctx)) break;
-          mbar_expect_tx(bar_q_full + 8 * t, parts * Cfg::kQBytes, issue);
-          for (uint32_t part = 0; part < parts; ++part)
+          mbar_expect_tx(bar_q_full + 8 * t, 2 * Cfg::kQBytes, issue);
+          for (uint32_t part = 0; part < 2; ++part)
             load_queries(s_q + Cfg::q_at((uint32_t)t, part), &map_q, bar_q_full + 8 * t, q_row + BM * t, (int)part * args.n_kv_heads + kv_head, issue);
         } else if (issue) {
           mbar_arrive(bar_q_full + 8 * t);

@@ -1,10 +1,12 @@
 """The paged cache where it can go wrong, against plain float64 forms."""
+import math
+
 import numpy as np
 import pytest
 import torch
 
 from paper_2404_09529_b200.runner import PagedDecoder
-from test_paged import BF16, E4M3, Pages, check_step, host64, new_rows
+from test_paged import BF16, E4M3, Pages, check_step, host64, new_rows, rotate64, shared_case
 
 
 # ------------------------------------------------------------------------------------------
@@ -53,3 +55,90 @@ def test_8_bit_step_over_values_of_a_small_scale(v_scale, hq, hkv, d, prompts):
         # Weights are 1. Sums in fp32, twice 2^-24 a term for tensor cores that truncate, and a few roundings behind them; then half of
         # a step of bf16: 2^-8 of O, or 2^-134 where bf16 has no bits for more.
         assert (np.abs(got[i] - want) <= (n + 16) * 2.0 ** -23 * mean + np.abs(want) * 2.0 ** -8 + 2.0 ** -134).all(), i
+
+
+# ------------------------------------------------------------------------------------------
+# How exact the shared rows are
+# ------------------------------------------------------------------------------------------
+# Queries reach the products as two bf16 numbers each, 2^-16, their weights as one.
+def attend_shared(q, keys, values, scale):
+    """O [heads, d] of queries of one KV head, and how far it may be off. e: what a score may be off by, from the query's parts, its
+    rotation in fp32 (3 roundings) and a sum of 2 d products in fp32, twice that for tensor cores that truncate; a weight over their sum
+    is then off by a factor of exp(2 e) at most, and by 2^-8 as one bf16 number, 2^-22 of its exponential and n 2^-23 of the sums. All of
+    it times sum p |v|, and the last rounding, 2^-8 of O."""
+    s = keys @ q.T * scale                             # [n, heads]
+    p = np.exp(s - s.max(0))
+    p /= p.sum(0)
+    o, mean = p.T @ values, p.T @ np.abs(values)
+    size = (np.abs(keys) @ np.abs(q).T).max(0) * abs(scale)
+    d, n = q.shape[1], len(keys)
+    e = size * (2.0 ** -16 + (4 * d + 8) * 2.0 ** -24) + 2.0 ** -22
+    err = mean * (np.exp(2 * e) - 1 + 2.0 ** -8 + n * 2.0 ** -23 + 64 * 2.0 ** -23)[:, None]
+    return o, np.abs(o) * 2.0 ** -8 + err * (1 + 2.0 ** -8)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("samples,hq,hkv,d,page", [(5, 4, 4, 64, 16), (40, 8, 1, 64, 32), (16, 8, 1, 128, 16), (3, 2, 2, 128, 64), (48, 16, 2, 128, 16)])
+def test_queries_over_shared_rows_keep_their_lower_part(samples, hq, hkv, d, page):
+    """Keys whose products with the queries cancel but for what a query loses as one bf16 number: k = +-c (q~_b, -q~_a) at elements
+    a and b, with q~ the rounded query. The scores are then +-1 to +-4 with both parts and 0 with one."""
+    shared, n = 512, 520
+    P, lengths, g = shared_case([(shared, [n] * samples)], hq, hkv, d, page, False, False, seed=d + samples, poison=False)
+    rng = np.random.default_rng(samples)
+    raw = torch.from_numpy(rng.standard_normal((hkv, d))).to(BF16)
+    turned = rotate64(host64(raw)[None], [n - 1], 10000.0)[0]
+    rounded = host64(torch.from_numpy(turned).float().to(BF16))
+    scale, sign = 1 / math.sqrt(d), np.where(rng.random(shared) < 0.5, -1.0, 1.0)
+    ids = torch.from_numpy(P.table[0, :shared // page].astype(np.int64))
+    keys = torch.from_numpy(0.05 * rng.standard_normal((shared, hkv, d)))
+    values = torch.from_numpy(0.1 * rng.standard_normal((shared, hkv, d)) + sign[:, None, None])
+    for h in range(hkv):
+        cross = np.outer(turned[h], rounded[h]) - np.outer(rounded[h], turned[h])      # q_a q~_b - q_b q~_a
+        a, b = np.unravel_index(np.abs(cross).argmax(), cross.shape)
+        c = 2.0 ** np.ceil(np.log2(1 / (abs(cross[a, b]) * scale)))                    # scores of 1 to 2
+        keys[:, h, [a, b]] = torch.from_numpy(np.outer(sign, 2 * c * np.array([rounded[h, b], -rounded[h, a]])))
+    for pool, rows in zip(P.pools, (keys, values)):
+        pool[ids] = rows.to(BF16).view(-1, page, hkv, d).transpose(1, 2)
+    caches = P.cuda()
+    q = raw.repeat_interleave(hq // hkv, 0).expand(samples, hq, d).contiguous().cuda()
+    dec = PagedDecoder(caches, hq, 10000.0)
+    got = host64(dec.step(torch.from_numpy(lengths).cuda(), q, groups=g))
+    assert dec.device_status() == 0
+    for i in range(samples):
+        k, v = (P.rows(w, i, n) for w in (0, 1))
+        for h in range(hkv):
+            per = hq // hkv
+            o, tol = attend_shared(turned[h][None], k[:, h], v[:, h], scale)
+            lossy = attend_shared(rounded[h][None], k[:, h], v[:, h], scale)[0]
+            assert (np.abs(o - lossy) > 4 * tol).mean() > 0.9          # (a query of one part would be seen)
+            for m in range(per):
+                assert (np.abs(got[i, h * per + m] - o[0]) <= tol[0]).all(), (i, h, m)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("groups,hq,hkv,d,page,softmax_scale,outside", [
+    ([(320 + 64 * g, [700 + 3 * i + g for i in range(8)]) for g in range(5)], 32, 32, 128, 64, 0.0, ()),      # 1280 query heads: a warp joins each
+    ([(1000, [1000 + i for i in range(40)])], 32, 8, 128, 16, 0.05, (3, -1, 0, 200)),                         # 160 query rows of a KV head
+    ([(256, [256 + i for i in range(17)])], 8, 1, 128, 128, 0.0, ()),                                         # 136 rows: a second tile of 8
+    ([(256, [300] * 16), (512, [513, -1, 600])], 8, 1, 128, 32, 0.2, ()),
+    ([(2000, [2100 + i for i in range(33)])], 8, 1, 128, 16, 0.0, ()),                                        # 264 rows: both tiles, and a split item of 8
+    ([(512, [520 + i for i in range(40)]), (48, [60] * 3)], 8, 2, 64, 16, 0.25, (77,)),
+])
+def test_shared_step_within_its_roundings(groups, hq, hkv, d, page, softmax_scale, outside):
+    """Every element of O within what the roundings that there are can do, at the softmax scales that a model may have."""
+    P, lengths, g = shared_case(groups, hq, hkv, d, page, True, False, seed=hq + d, outside=outside)
+    caches = P.cuda()
+    q = new_rows(len(lengths), hq, hkv, d, 31, True)[0]
+    dec = PagedDecoder(caches, hq, 10000.0, softmax_scale=softmax_scale)
+    got = host64(dec.step(torch.from_numpy(lengths).cuda(), q, groups=g))
+    assert dec.device_status() == 0
+    per = hq // hkv
+    for i, n in enumerate(int(x) for x in lengths):
+        if n <= 0:
+            assert not got[i].any()
+            continue
+        turned = rotate64(host64(q[i:i + 1]), [n - 1], 10000.0)[0]
+        k, v = (P.rows(w, i, n) for w in (0, 1))
+        for h in range(hq):
+            o, tol = attend_shared(turned[h:h + 1], k[:, h // per], v[:, h // per], softmax_scale or 1 / math.sqrt(d))
+            assert (np.abs(got[i, h] - o[0]) <= tol[0]).all(), (i, h)
