@@ -348,7 +348,7 @@ int pp_paged_append(const pp_attn_params* params, const pp_paged_cache* cache, c
                     int32_t* device_status, void* stream);
 
 /*
- * pp_decode_step over a paged cache: one generation step for up to 8192 prompts.
+ * pp_decode_step over a paged cache: one generation step for up to 8192 prompts (more: several calls, on parts of the table).
  * With k_new and v_new: the new token of prompt i sits at position lengths[i]; its query and key are rotated by that position,
  * key and value are appended at row lengths[i], and the query attends to rows 0 .. lengths[i], as the pages hold them.
  * With both NULL: the pages hold the token already. The query sits at position lengths[i] - 1 and attends to rows

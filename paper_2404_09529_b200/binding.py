@@ -19,6 +19,8 @@ PP_FLAG_KEEP_ROPE_TABLE = 4
 # Types of the pages of a paged cache, and what the paged calls leave in the status word.
 PP_CACHE_BF16, PP_CACHE_E4M3 = 0, 1
 PP_PAGED_BAD_PROMPT, PP_PAGED_BAD_POSITION, PP_PAGED_BAD_PAGE, PP_PAGED_BAD_LENGTH, PP_PAGED_BAD_GROUPS = range(201, 206)
+# Prompts of one generation step over a paged cache (kMaxPagedPrompts of the library).
+PP_PAGED_MAX_PROMPTS = 8192
 # Tables of at most this many int32 words travel as kernel parameters in the independent mode (kInlineInts of the library).
 PARAMETER_TABLE_INTS = 896
 

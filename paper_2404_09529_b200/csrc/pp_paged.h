@@ -13,7 +13,7 @@
 
 namespace pp {
 
-constexpr int kMaxPagedPrompts = 8192;   // a step's block sums one number per prompt in shared memory
+constexpr int kMaxPagedPrompts = 8192;   // and groups, of which the block that lays the shared work out holds three numbers each in shared memory
 constexpr int kSharedTileRows = 256;     // query rows of a work item of the shared rows: two tiles of 128
 constexpr int kSharedTileKeys = 128;
 

@@ -455,7 +455,8 @@ class PagedDecoder:
         """One token for each prompt of the table's first len(lengths) rows. lengths: int32 on the device, rows that the pages hold
         (< 0: no prompt). q [n, Hq, D]; k, v [n, Hkv, D]: the new token, appended; or None: the pages hold it. groups: (group_ptr,
         shared_len), int32 on the device, where prompts share their first pages. Returns out [n, Hq, D]; on the
-        current stream, asynchronous, nothing is read back. The lengths are the caller's to advance."""
+        current stream, asynchronous, nothing is read back. The lengths are the caller's to advance. More than 8192 prompts are
+        the work of several calls of the library; groups may lie across them, but there are no more groups than prompts of a call."""
         c = self.caches
         n = c.check_ints(lengths, "lengths")
         if not 0 < n <= c.n_prompts:
@@ -477,8 +478,15 @@ class PagedDecoder:
                 raise ValueError("groups: group_ptr has one entry more than shared_len")
             if n_groups == 0:
                 groups = None
+        calls = -(-n // B.PP_PAGED_MAX_PROMPTS)
+        if groups is not None and calls > 1:
+            least = n - (calls - 1) * -(-n // calls)   # prompts of the last call
+            if n_groups > least:
+                raise ValueError(f"groups: no more than {least} for {n} prompts")
         with on_device(c.device):
-            if groups is None:
+            if calls > 1:
+                self._step_in_parts(calls, lengths, n, q, q_stride, k, k_stride, v, v_stride, out, groups)
+            elif groups is None:
                 ws, size = self._workspace(n, 0)
                 B.pp_paged_decode_step(self.params, c.struct, lengths, n, q, q_stride, k, k_stride, v, v_stride, out, ws, size, self.status,
                                        B.current_stream())
@@ -487,6 +495,26 @@ class PagedDecoder:
                 B.pp_paged_decode_shared(self.params, c.struct, lengths, n, ptr, shared, n_groups, q, q_stride, k, k_stride, v, v_stride, out,
                                          ws, size, self.status, B.current_stream())
         return out
+
+    def _step_in_parts(self, calls, lengths, n, q, q_stride, k, k_stride, v, v_stride, out, groups) -> None:
+        """`step` as so many calls, each for the prompts of a part of the table."""
+        c, stream = self.caches, B.current_stream()
+        most = -(-n // calls)
+        ws, size = self._workspace(most, 0 if groups is None else groups[1].shape[0])
+        if groups is not None:
+            ptr, shared = groups
+            bad = (ptr[1:] < ptr[:-1]).any() | (ptr[0] < 0) | (ptr[-1] > n)     # for all parts, whichever of them would show it
+        for a in range(0, n, most):
+            b = min(a + most, n)
+            part = B.PagedCache.from_buffer_copy(c.struct)
+            part.page_table += a * 4 * c.struct.table_stride
+            new = (None if x is None else x[a:b] for x in (k, v))
+            args = (q[a:b], q_stride, next(new), k_stride, next(new), v_stride, out[a:b], ws, size, self.status, stream)
+            if groups is None:
+                B.pp_paged_decode_step(self.params, part, lengths[a:b], b - a, *args)
+            else:
+                B.pp_paged_decode_shared(self.params, part, lengths[a:b], b - a, torch.where(bad, -1, ptr.clamp(a, b) - a), shared,
+                                         shared.shape[0], *args)
 
     def device_status(self) -> int:
         return int(self.status.item())

@@ -5,7 +5,8 @@ import numpy as np
 import pytest
 import torch
 
-from paper_2404_09529_b200.runner import PagedDecoder
+import paper_2404_09529_b200 as pp
+from paper_2404_09529_b200.runner import PagedCaches, PagedDecoder
 from test_paged import BF16, E4M3, Pages, check_step, host64, new_rows, rotate64, shared_case
 
 
@@ -142,3 +143,90 @@ def test_shared_step_within_its_roundings(groups, hq, hkv, d, page, softmax_scal
         for h in range(hq):
             o, tol = attend_shared(turned[h:h + 1], k[:, h // per], v[:, h // per], softmax_scale or 1 / math.sqrt(d))
             assert (np.abs(got[i, h] - o[0]) <= tol[0]).all(), (i, h)
+
+
+# ------------------------------------------------------------------------------------------
+# More prompts than one call takes
+# ------------------------------------------------------------------------------------------
+def _one_page_each(k, hq, hkv, d, page, sharing, seed):
+    """k prompts of up to `page` rows in a page of their own, behind a page that each `sharing` of them have in common."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    firsts = -(-k // sharing)
+    at = torch.arange(k, device="cuda", dtype=torch.int32)
+    table = torch.stack([at // sharing, firsts + at], 1).contiguous()
+    pools = [torch.randn((firsts + k, hkv, page, d), device="cuda", dtype=BF16, generator=g) for _ in range(2)]
+    lengths = torch.randint(page, 2 * page, (k,), dtype=torch.int32, device="cuda", generator=g)
+    lengths[::97] = -1
+    q, kn, vn = (torch.randn((k, h, d), device="cuda", dtype=BF16, generator=g) for h in (hq, hkv, hkv))
+    return PagedCaches(*pools, table), lengths, q, kn, vn
+
+
+def _check_every_prompt(caches, n_rows, q, out, shared):
+    """O of every prompt (n_rows that it attends to, < 0: none, O is 0) against the float64 form, over the pages as they are."""
+    k, hq, d = q.shape
+    page, active = caches.page_size, n_rows >= 0
+    assert bool((out[~active] == 0).all())
+    n = n_rows.clamp(min=1)
+    rows = [x[caches.page_table.long()].movedim(2, 1).reshape(k, caches.hkv, -1, d).double() for x in (caches.k_pages, caches.v_pages)]
+    theta = 10000.0 ** (-torch.arange(d // 2, device="cuda", dtype=torch.float64) / (d // 2))
+    angle = ((n - 1).double()[:, None] * theta)[:, None]
+    a, b = q.double()[..., :d // 2], q.double()[..., d // 2:]
+    turned = torch.cat([a * angle.cos() - b * angle.sin(), b * angle.cos() + a * angle.sin()], -1).view(k, caches.hkv, -1, d)
+    s = torch.einsum("kgmd,kgrd->kgmr", turned, rows[0]) / math.sqrt(d)
+    s = s.masked_fill(torch.arange(s.shape[-1], device="cuda") >= n[:, None, None, None], -math.inf)
+    p = torch.softmax(s, -1)
+    want = torch.einsum("kgmr,kgrd->kgmd", p, rows[1])
+    # O is rounded to bf16 once: 2^-8 of it. A query reaches the products as two bf16 numbers (2^-16 of it), 2^-17 for the rotation and a sum
+    # of 64 products in fp32: that moves a score by at most e = (that) sum |q k| scale, and so a weight over the sum of them by a factor of
+    # exp(2 e) at most. A weight is one bf16 number over shared rows (2^-8 of it), else two (2^-15); 2^-17 for the sums over a few dozen
+    # rows in fp32. All of it times sum p |v|.
+    part = 2.0 ** -8 if shared else 2.0 ** -15
+    e = torch.einsum("kgmd,kgrd->kgmr", turned.abs(), rows[0].abs()).amax(-1, keepdim=True) / math.sqrt(d) * (2.0 ** -16 + 2.0 ** -17)
+    err = torch.einsum("kgmr,kgrd->kgmd", p, rows[1].abs()) * (torch.exp(2 * e) - 1 + part + 2.0 ** -17) * (1 + part)
+    tol = want.abs() * 2.0 ** -8 + err * (1 + 2.0 ** -8)
+    off = ((out.double().view_as(want) - want).abs() <= tol).flatten(1).all(1) | ~active
+    assert bool(off.all()), (~off).nonzero()[:8]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fresh", [True, False])
+@pytest.mark.parametrize("k,sharing", [(16384, 0), (16384, 256), (8193, 300), (20000, 6000), (8192, 64)])
+def test_step_of_more_prompts_than_a_call_takes(k, sharing, fresh):
+    """Up to 64 groups of 256 samples, groups that lie on both sides of a cut, rows of no prompt: O of every prompt, and the pages are those
+    that an append of the same rows leaves."""
+    hq, hkv, d, page = 2, 1, 64, 16
+    caches, lengths, q, kn, vn = _one_page_each(k, hq, hkv, d, page, sharing or 1, seed=k + sharing)
+    pools = caches.k_pages.clone(), caches.v_pages.clone()
+    groups = None
+    if sharing:
+        starts = list(range(0, k, sharing)) + [k]
+        groups = tuple(torch.tensor(x, dtype=torch.int32, device="cuda") for x in (starts, [page] * (len(starts) - 1)))
+    dec = PagedDecoder(caches, hq, 10000.0)
+    out = dec.step(lengths, q, *((kn, vn) if fresh else (None, None)), groups=groups)
+    assert dec.device_status() == 0
+    _check_every_prompt(caches, lengths + fresh * (lengths >= 0).int(), q, out, bool(sharing))
+    if fresh:
+        again = PagedCaches(*pools, caches.page_table)
+        prompt = torch.arange(k, dtype=torch.int32, device="cuda")
+        again.append(torch.where(lengths >= 0, prompt, torch.full_like(prompt, -1)), lengths, kn, vn, 10000.0)
+    assert torch.equal(caches.k_pages, pools[0]) and torch.equal(caches.v_pages, pools[1])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bad", [[0, 9000, 100, 16384], [0, 6000, 5000, 16384], [-1, 100, 200, 300], [0, 1, 2, 16385]])
+def test_bad_groups_of_more_prompts_than_a_call_takes(bad):
+    """Said to be bad for all of the prompts, whichever part of them a call is made for: nothing is shared."""
+    hq, hkv, d, page, k = 2, 1, 64, 16, 16384
+    caches, lengths, q, _, _ = _one_page_each(k, hq, hkv, d, page, 1, seed=9)
+    groups = torch.tensor(bad, dtype=torch.int32, device="cuda"), torch.full((3,), page, dtype=torch.int32, device="cuda")
+    dec = PagedDecoder(caches, hq, 10000.0)
+    out = dec.step(lengths, q, groups=groups)
+    assert dec.device_status() == pp.PP_PAGED_BAD_GROUPS
+    _check_every_prompt(caches, lengths, q, out, False)
+
+
+def test_more_groups_than_prompts_of_a_call_are_refused():
+    caches = PagedCaches(*(torch.zeros(1, 1, 16, 64, dtype=BF16) for _ in range(2)), torch.zeros(9000, 1, dtype=torch.int32))
+    ints = lambda n: torch.zeros(n, dtype=torch.int32)
+    with pytest.raises(ValueError, match="groups"):
+        PagedDecoder(caches, 1, 10000.0).step(ints(9000), torch.zeros(9000, 1, 64, dtype=BF16), groups=(ints(4502), ints(4501)))
