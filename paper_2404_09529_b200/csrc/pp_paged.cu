@@ -98,8 +98,8 @@ append_kernel(const __grid_constant__ AppendArgs a) {
   const int64_t row0 = (int64_t)blockIdx.x * a.rows_per_cta;
   const int rows = (int)min((int64_t)a.rows_per_cta, a.n_rows - row0), head0 = blockIdx.y * a.heads_per_cta;
   const int units = min(a.heads_per_cta, a.n_kv_heads - head0) * kUnits;
-  pdl_launch_dependents();
   pdl_wait();
+  pdl_launch_dependents();              // (not before the wait: a step reads ahead what lies two kernels back, see below)
   for (int u0 = 0; u0 < rows * units; u0 += kAppendThreads) {
     const int u = u0 + tid, r = u / units, w = u - r * units + head0 * kUnits, head = w / kUnits, c = 8 * (w - head * kUnits);
     int prompt = -1, pos = 0;
@@ -205,8 +205,8 @@ append_kernel(const __grid_constant__ AppendArgs a) {
 // of a KV head as the 8 columns, absent heads 0. Over bf16 pages a query and a weight each reach it as the sum of two
 // 16-bit numbers: HBM leaves the tensor cores idle, and scores and O are then exact to 2^-16, far below O's last rounding of 2^-8.
 // The lengths live on the device: every CTA sums them itself, and the grid and the room for parts depend on neither them nor k.
-// (It does so before its wait for the kernel in front, which, like all kernels here, lets the next one start only after its own wait:
-// what that one waited for is there then. Not through L1, which may hold what it was before.)
+// (It does so before its wait for the kernel in front, which, like all kernels of this file and pp_paged_shared.cu, lets the next one start
+// only after its own wait: what that one waited for is there then. Not through L1, which may hold what it was before.)
 constexpr int kMaxGroup = 8;            // query heads per KV head: the N of the tensor-core product
 constexpr int kMostStepWarps = 7, kMostPieces = kSms * kMostStepWarps;
 constexpr int kHalfUnit = 4096;         // bytes of K, and of V, in a unit

@@ -1,5 +1,6 @@
 """The paged cache where it can go wrong, against plain float64 forms."""
 import math
+import os
 
 import numpy as np
 import pytest
@@ -230,3 +231,19 @@ def test_more_groups_than_prompts_of_a_call_are_refused():
     ints = lambda n: torch.zeros(n, dtype=torch.int32)
     with pytest.raises(ValueError, match="groups"):
         PagedDecoder(caches, 1, 10000.0).step(ints(9000), torch.zeros(9000, 1, 64, dtype=BF16), groups=(ints(4502), ints(4501)))
+
+
+# ------------------------------------------------------------------------------------------
+# Kernels one behind the other
+# ------------------------------------------------------------------------------------------
+def test_no_kernel_lets_the_next_one_start_before_its_own_wait():
+    """What the step reads ahead of its wait (lengths, table, rows that were there) is complete only because of that."""
+    seen = 0
+    for name in ("pp_paged.cu", "pp_paged_shared.cu"):
+        with open(os.path.join(os.path.dirname(pp.__file__), "csrc", name)) as f:
+            lines = [line.split("//")[0].strip() for line in f]
+        for at, line in enumerate(lines):
+            if line == "pdl_launch_dependents();":
+                seen += 1
+                assert lines[at - 1] == "pdl_wait();", (name, at + 1)
+    assert seen == 6
