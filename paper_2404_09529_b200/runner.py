@@ -391,15 +391,28 @@ class PagedCaches:
             B.pp_paged_append(params, self.struct, prompt, position, rows, self.n_prompts, k_new, k_stride, v_new, v_stride,
                               self.status, B.current_stream())
 
-    def append_prefill(self, prefill: PrefillBatch) -> torch.Tensor:
+    def append_prefill(self, prefill: PrefillBatch, start=0) -> torch.Tensor:
         """UNPACK into pages: the rotated keys and the values of a PrefillBatch that has run, prompt i of the batch into
-        prompt i here (`reserve` its rows first). Returns the lengths, int32 on the device."""
+        prompt i here (`reserve` its rows first). start (int or one int per prompt): rows before it are left as they are, such as
+        those in pages from `share`, which other prompts may be reading and which every prompt that has them would write. Returns
+        the lengths, int32 on the device."""
+        if (prefill.hkv, prefill.d) != (self.hkv, self.d):
+            raise ValueError(f"the prefill has {prefill.hkv} KV heads of {prefill.d}, the caches {self.hkv} of {self.d}")
+        if prefill.k > self.n_prompts:
+            raise ValueError(f"{prefill.k} prompts, {self.n_prompts} rows of the page table")
+        room = self.struct.table_stride if self._count is None else self._count[:prefill.k]
+        short = np.nonzero(-(-prefill.lengths.astype(np.int64) // self.page_size) > room)[0]
+        if len(short):
+            raise ValueError(f"prompt {short[0]} has no pages for its {prefill.lengths[short[0]]} rows")
+        start = np.broadcast_to(np.asarray(start, dtype=np.int64), (prefill.k,))
+        if (start < 0).any() or (start > prefill.lengths).any():
+            raise ValueError("start: rows that the prompts have")
         segment = np.full((prefill.pack.n_bins, prefill.pack.capacity), -1, dtype=np.int32)
         position = np.zeros_like(segment)
         for i, n in enumerate(prefill.lengths):
-            at = slice(int(prefill.off_of[i]), int(prefill.off_of[i]) + int(n))
+            at = slice(int(prefill.off_of[i]) + int(start[i]), int(prefill.off_of[i]) + int(n))
             segment[prefill.bin_of[i], at] = i
-            position[prefill.bin_of[i], at] = np.arange(n)
+            position[prefill.bin_of[i], at] = np.arange(start[i], n)
         segment, position = (torch.from_numpy(x.reshape(-1)).to(self.device) for x in (segment, position))
         rows = segment.shape[0]
         self.append(segment, position, prefill.kk.view(rows, self.hkv, self.d), prefill.v.view(rows, self.hkv, self.d),

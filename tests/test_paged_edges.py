@@ -1,14 +1,15 @@
 """The paged cache where it can go wrong, against plain float64 forms."""
 import math
 import os
+from types import SimpleNamespace
 
 import numpy as np
 import pytest
 import torch
 
 import paper_2404_09529_b200 as pp
-from paper_2404_09529_b200.runner import PagedCaches, PagedDecoder
-from test_paged import BF16, E4M3, Pages, check_step, host64, new_rows, rotate64, shared_case
+from paper_2404_09529_b200.runner import PagedCaches, PagedDecoder, PrefillBatch
+from test_paged import BF16, E4M3, Pages, check_step, host64, new_rows, normal, rotate64, shared_case
 
 
 # ------------------------------------------------------------------------------------------
@@ -231,6 +232,63 @@ def test_more_groups_than_prompts_of_a_call_are_refused():
     ints = lambda n: torch.zeros(n, dtype=torch.int32)
     with pytest.raises(ValueError, match="groups"):
         PagedDecoder(caches, 1, 10000.0).step(ints(9000), torch.zeros(9000, 1, 64, dtype=BF16), groups=(ints(4502), ints(4501)))
+
+
+# ------------------------------------------------------------------------------------------
+# From the prefill into pages
+# ------------------------------------------------------------------------------------------
+def _prefill(lengths, hkv, d):
+    """What `append_prefill` looks at before it makes a call."""
+    return SimpleNamespace(hkv=hkv, d=d, k=len(lengths), lengths=np.array(lengths, np.int32))
+
+
+def test_a_prefill_that_does_not_fit_is_refused():
+    caches = PagedCaches.allocate(3, 20, 100, 8, 64, page_size=16, device="cpu")
+    for i, rows in enumerate((40, 100, 0)):
+        caches.reserve(i, rows)
+    table = PagedCaches(caches.k_pages, caches.v_pages, caches.page_table)     # (the table is the caller's: up to its rows' ends)
+    for c, lengths, hkv, d, start, says in [
+        (caches, [5, 5], 4, 128, 0, "heads"), (caches, [5, 5], 8, 128, 0, "heads"), (caches, [5, 5], 4, 64, 0, "heads"),
+        (caches, [1, 1, 0, 0], 8, 64, 0, "4 prompts"), (caches, [49, 100], 8, 64, 0, "prompt 0"), (caches, [48, 100, 1], 8, 64, 0, "prompt 2"),
+        (table, [5, 113], 8, 64, 0, "prompt 1"), (caches, [5, 5], 8, 64, 6, "start"), (caches, [5, 5], 8, 64, [0, -1], "start"),
+        (caches, [5, 5], 8, 64, [0, 0, 0], "shape"),
+    ]:
+        with pytest.raises(ValueError, match=says):
+            c.append_prefill(_prefill(lengths, hkv, d), start)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("mode", ["packed", "padded"])
+def test_a_prefill_leaves_rows_before_its_start(mode):
+    """Prompts behind a prefix: the first one's pages are shared, and the others' prefill leaves them as they are. In all of them stand the
+    bits that an append of every row leaves."""
+    lengths, hq, hkv, d, page = np.array([70, 33, 48, 90], np.int32), 4, 2, 64, 16
+    pre = PrefillBatch(lengths, hq, hkv, d, 10000.0, mode=mode)
+    pre.load(*(normal((int(lengths.sum()), h, d), s) for s, h in enumerate((hq, hkv, hkv))))
+    pre.run_fused()
+    whole, behind = (PagedCaches.allocate(4, 30, 100, hkv, d, page) for _ in range(2))
+    for i, n in enumerate(lengths):
+        whole.reserve(i, int(n))
+    assert torch.equal(whole.append_prefill(pre).cpu(), torch.from_numpy(lengths))
+    behind.reserve(0, 70)
+    start = [0]
+    for i in range(1, 4):
+        start.append(behind.share(0, i, 40))
+        behind.reserve(i, int(lengths[i]))
+    assert start == [0, 32, 32, 32]
+    shared = behind.page_table[0, :2].long()
+    for pool in (behind.k_pages, behind.v_pages):
+        pool[shared] = 7
+    behind.append_prefill(pre, [32, 32, 32, 32])
+    assert all(bool((pool[shared] == 7).all()) for pool in (behind.k_pages, behind.v_pages))
+    behind.append_prefill(pre, np.array(start))
+    assert int(whole.status) == int(behind.status) == 0
+    for a, b in ((whole.k_pages, behind.k_pages), (whole.v_pages, behind.v_pages)):
+        for i, n in enumerate(int(x) for x in lengths):
+            first = 0 if i == 0 else 2
+            rows = lambda pool, c: pool[c.page_table[i, first:-(-n // page)].long()].transpose(1, 2).reshape(-1, hkv, d)[:n - first * page]
+            assert torch.equal(rows(a, whole), rows(b, behind)) and bool(rows(a, whole).any() or i == 1)
+        assert torch.equal(a[whole.page_table[0, :2].long()], b[shared])
 
 
 # ------------------------------------------------------------------------------------------
