@@ -419,6 +419,14 @@ class PagedCaches:
                     prefill.rope_base, rotated=True)
         return torch.from_numpy(prefill.lengths).to(self.device)
 
+    def device_status(self) -> int:
+        """What the appends found wrong first (PP_PAGED_*), or 0: waits for them. It stays until `reset_status`."""
+        return int(self.status.item())
+
+    def reset_status(self) -> None:
+        """On the current stream: appends queued behind it report anew."""
+        self.status.zero_()
+
 
 class _Nothing:
     def __enter__(self):
@@ -509,6 +517,14 @@ class PagedDecoder:
                                          ws, size, self.status, B.current_stream())
         return out
 
+    def device_status(self) -> int:
+        """What the steps found wrong first (PP_PAGED_*, or a wait that gave up), or 0: waits for them. It stays until `reset_status`."""
+        return int(self.status.item())
+
+    def reset_status(self) -> None:
+        """On the current stream: steps queued behind it report anew."""
+        self.status.zero_()
+
     def _step_in_parts(self, calls, lengths, n, q, q_stride, k, k_stride, v, v_stride, out, groups) -> None:
         """`step` as so many calls, each for the prompts of a part of the table."""
         c, stream = self.caches, B.current_stream()
@@ -528,6 +544,3 @@ class PagedDecoder:
             else:
                 B.pp_paged_decode_shared(self.params, part, lengths[a:b], b - a, torch.where(bad, -1, ptr.clamp(a, b) - a), shared,
                                          shared.shape[0], *args)
-
-    def device_status(self) -> int:
-        return int(self.status.item())

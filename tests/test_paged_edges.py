@@ -305,3 +305,36 @@ def test_no_kernel_lets_the_next_one_start_before_its_own_wait():
                 seen += 1
                 assert lines[at - 1] == "pdl_wait();", (name, at + 1)
     assert seen == 6
+
+
+# ------------------------------------------------------------------------------------------
+# Status words
+# ------------------------------------------------------------------------------------------
+def test_status_words_are_read_and_reset():
+    caches = PagedCaches.allocate(2, 4, 32, 1, 64, page_size=16, device="cpu")
+    for x in (caches, PagedDecoder(caches, 1, 10000.0)):
+        assert x.device_status() == 0
+        x.status.fill_(pp.PP_PAGED_BAD_PAGE)
+        assert x.device_status() == pp.PP_PAGED_BAD_PAGE == x.device_status()
+        x.reset_status()
+        assert x.device_status() == 0
+
+
+@pytest.mark.gpu
+def test_a_reset_status_word_tells_of_the_next_mistake():
+    caches = PagedCaches.allocate(2, 4, 32, 1, 64, page_size=16)
+    caches.reserve(0, 32)
+    _, k, v = new_rows(1, 1, 1, 64, 3, False)
+    one = lambda x: torch.tensor([x], dtype=torch.int32, device="cuda")
+    dec = PagedDecoder(caches, 1, 10000.0)
+    for prompt, position, code in ((5, 0, pp.PP_PAGED_BAD_PROMPT), (0, 32, pp.PP_PAGED_BAD_POSITION), (0, 31, 0), (1, 0, pp.PP_PAGED_BAD_PAGE)):
+        caches.append(one(prompt), one(position), k, v, 10000.0)
+        assert caches.device_status() == code
+        caches.append(one(7), one(0), k, v, 10000.0)
+        assert caches.device_status() == (code or pp.PP_PAGED_BAD_PROMPT)            # the first one stays
+        caches.reset_status()
+    q = new_rows(2, 1, 1, 64, 4, False)[0]
+    for lengths, code in (([40, -1], pp.PP_PAGED_BAD_LENGTH), ([32, -1], 0), ([5, 5], pp.PP_PAGED_BAD_PAGE)):
+        dec.step(torch.tensor(lengths, dtype=torch.int32, device="cuda"), q)
+        assert dec.device_status() == code
+        dec.reset_status()
