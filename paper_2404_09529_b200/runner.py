@@ -293,7 +293,8 @@ class PagedCaches:
     def allocate(cls, n_prompts: int, n_pages: int, max_rows: int, n_kv_heads: int, head_dim: int, page_size: int = 64,
                  dtype: torch.dtype = torch.bfloat16, rows_first: bool = False, device: str = "cuda",
                  k_scale: torch.Tensor | None = None, v_scale: torch.Tensor | None = None) -> "PagedCaches":
-        """Pools of n_pages zeroed pages and an empty table for n_prompts prompts of up to max_rows rows."""
+        """Pools of n_pages zeroed pages and an empty table for n_prompts prompts of up to max_rows rows. The further layers of a
+        model need no table of their own: PagedCaches(k_pages, v_pages, first.page_table), with pools of the same number of pages."""
         shape = (n_pages, page_size, n_kv_heads, head_dim) if rows_first else (n_pages, n_kv_heads, page_size, head_dim)
         pools = [torch.zeros(shape, dtype=torch.uint8 if dtype.itemsize == 1 else torch.bfloat16, device=device).view(dtype) for _ in range(2)]
         table = torch.full((n_prompts, -(-max_rows // page_size)), -1, dtype=torch.int32, device=device)
@@ -446,7 +447,8 @@ def on_device(device: torch.device):
 
 class PagedDecoder:
     """Generation steps over PagedCaches through pp_paged_decode_step / pp_paged_decode_shared. Owns the workspace (of the steps
-    of one stream: steps that may run at the same time want a decoder each) and the status word."""
+    of one stream: steps that may run at the same time want a decoder each) and the status word: to be kept until the steps that
+    were queued have run, and as long as a graph that captured some."""
 
     def __init__(self, caches: PagedCaches, n_q_heads: int, rope_base: float, softmax_scale: float = 0.0):
         self.caches, self.hq = caches, n_q_heads

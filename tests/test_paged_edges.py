@@ -1,4 +1,5 @@
-"""The paged cache where it can go wrong, against plain float64 forms."""
+"""The paged cache where it can go wrong: scales of the smallest sizes, batches of more prompts than one call takes, prefills that do not fit,
+how exact the shared rows are, calls one behind the other; against plain float64 forms."""
 import math
 import os
 from types import SimpleNamespace
@@ -58,6 +59,36 @@ def test_8_bit_step_over_values_of_a_small_scale(v_scale, hq, hkv, d, prompts):
         # Weights are 1. Sums in fp32, twice 2^-24 a term for tensor cores that truncate, and a few roundings behind them; then half of
         # a step of bf16: 2^-8 of O, or 2^-134 where bf16 has no bits for more.
         assert (np.abs(got[i] - want) <= (n + 16) * 2.0 ** -23 * mean + np.abs(want) * 2.0 ** -8 + 2.0 ** -134).all(), i
+
+
+# ------------------------------------------------------------------------------------------
+# Appending: rows whose heads go round a block's loop
+# ------------------------------------------------------------------------------------------
+@pytest.mark.gpu
+@pytest.mark.parametrize("hkv,d,dtype,fused,rotated", [
+    (32, 128, BF16, True, False), (40, 128, E4M3, False, False), (33, 128, BF16, False, True), (48, 64, E4M3, True, False),
+])
+def test_append_of_many_wide_rows_is_that_of_few(hkv, d, dtype, fused, rotated):
+    """A row of more than 2048 elements is shared out to several blocks while few are appended, and is the work of one where there are
+    many: the same bits."""
+    rows, prompts, page = 1300, 7, 32
+    rng = np.random.default_rng(hkv)
+    prompt = rng.integers(-1, prompts, rows).astype(np.int32)
+    position = np.arange(rows, dtype=np.int32)         # (every cell once)
+    s = torch.full((hkv,), 0.03, device="cuda") if dtype == E4M3 else None
+    many, few = (PagedCaches.allocate(prompts, prompts * -(-rows // page), rows, hkv, d, page, dtype=dtype, k_scale=s, v_scale=s) for _ in range(2))
+    for c in (many, few):
+        for i in range(prompts):
+            c.reserve(i, rows)
+    prompt, position = (torch.from_numpy(x).cuda() for x in (prompt, position))
+    _, k, v = new_rows(rows, 1, hkv, d, 8, fused)
+    many.append(prompt, position, k, v, 10000.0, rotated=rotated)
+    for a in range(0, rows, 100):
+        few.append(prompt[a:a + 100], position[a:a + 100], k[a:a + 100], v[a:a + 100], 10000.0, rotated=rotated)
+    assert int(many.status) == int(few.status) == 0 and torch.equal(many.page_table, few.page_table)
+    raw = torch.uint8 if dtype == E4M3 else torch.int16
+    for a, b in ((many.k_pages, few.k_pages), (many.v_pages, few.v_pages)):
+        assert torch.equal(a.view(raw), b.view(raw)) and bool(a.view(raw).any())
 
 
 # ------------------------------------------------------------------------------------------
@@ -126,6 +157,8 @@ def test_queries_over_shared_rows_keep_their_lower_part(samples, hq, hkv, d, pag
     ([(256, [300] * 16), (512, [513, -1, 600])], 8, 1, 128, 32, 0.2, ()),
     ([(2000, [2100 + i for i in range(33)])], 8, 1, 128, 16, 0.0, ()),                                        # 264 rows: both tiles, and a split item of 8
     ([(512, [520 + i for i in range(40)]), (48, [60] * 3)], 8, 2, 64, 16, 0.25, (77,)),
+    ([(0, [20] * 20), (300, [310, 305, 420])], 8, 1, 128, 16, 0.0, ()),                                       # 160 rows that share nothing
+    ([(128, [130] * 40), (16, [30] * 2), (2100, [2200] * 2)], 8, 1, 128, 16, 0.0, (1,)),                      # one key tile; items of both kinds
 ])
 def test_shared_step_within_its_roundings(groups, hq, hkv, d, page, softmax_scale, outside):
     """Every element of O within what the roundings that there are can do, at the softmax scales that a model may have."""
@@ -338,3 +371,44 @@ def test_a_reset_status_word_tells_of_the_next_mistake():
         dec.step(torch.tensor(lengths, dtype=torch.int32, device="cuda"), q)
         assert dec.device_status() == code
         dec.reset_status()
+
+
+# ------------------------------------------------------------------------------------------
+# Captured steps, layers
+# ------------------------------------------------------------------------------------------
+@pytest.mark.gpu
+@pytest.mark.parametrize("prompts,sharing,hq,hkv,d", [(3, 3, 8, 1, 128), (40, 40, 8, 1, 128), (16, 8, 4, 4, 64), (9000, 300, 2, 1, 64), (9000, 0, 2, 1, 64)])
+def test_captured_step_is_the_step(prompts, sharing, hq, hkv, d):
+    """With few and many queries of a group, and of more prompts than one call takes: replays over new queries and lengths."""
+    caches, lengths, q, kn, vn = _one_page_each(prompts, hq, hkv, d, 16, sharing or 1, seed=prompts)
+    starts = list(range(0, prompts, sharing or prompts)) + [prompts]
+    groups = tuple(torch.tensor(x, dtype=torch.int32, device="cuda") for x in (starts, [16] * (len(starts) - 1))) if sharing else None
+    dec, eager = PagedDecoder(caches, hq, 10000.0), PagedDecoder(caches, hq, 10000.0)
+    out, g = torch.zeros_like(q), torch.cuda.CUDAGraph()
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        dec.step(lengths, q, kn, vn, out=out, groups=groups)
+    stream.synchronize()
+    with torch.cuda.graph(g, stream=stream):
+        dec.step(lengths, q, kn, vn, out=out, groups=groups)
+    for turn in range(3):
+        lengths.copy_(torch.where(lengths < 0, lengths, 16 + (lengths + 5 * turn) % 16))
+        for x in (q, kn, vn):
+            x.copy_(x.roll(turn + 1, 0))
+        out.zero_()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(stream):
+            g.replay()
+        stream.synchronize()
+        assert torch.equal(out, eager.step(lengths, q, kn, vn, groups=groups)) and bool(out.any())
+    assert dec.device_status() == eager.device_status() == 0
+
+
+def test_layers_share_a_table():
+    first = PagedCaches.allocate(2, 8, 60, 2, 64, page_size=16, device="cpu")
+    second = PagedCaches(torch.zeros_like(first.k_pages), torch.zeros_like(first.v_pages), first.page_table)
+    first.reserve(0, 40)
+    assert second.page_table is first.page_table and second.struct.page_table == first.struct.page_table
+    with pytest.raises(ValueError):
+        second.reserve(1, 16)                          # (pages are handed out in one place)
