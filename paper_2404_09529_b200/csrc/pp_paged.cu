@@ -54,9 +54,9 @@ __device__ __forceinline__ uint32_t round_e4m3(float a, float b, float c, float 
 // A copy with a rotation in it, bound by HBM: a CTA takes as many rows (or heads of one) as make 2048 elements of K. A thread has one
 // pair of 8-element pieces of K (c and D/2 + c) and two pieces of V of the same row, so that all it needs is that row's prompt and
 // position: its loads, the page's number and the angles (once for all heads of a row, through shared memory) are then under way together.
-// 17 554 rows of 32 heads of 128 take 89 to 92 us (6.3 TB/s and more; 114 with the row's place found first and handed round), 44 k short rows of
-// 8 heads of 64 into 8 bits 33 us (4.1 TB/s, was 55), where instructions count: 430 a thread, a quarter of them for the angle, and as
-// many for the conversions.
+// 17 554 rows of 32 heads of 128 take 90 to 92 us (6.2 to 6.4 TB/s; 114 us with the row's place found first and handed round), 44 k short
+// rows of 8 heads of 64 into 8 bits 33 us (4.1 TB/s, was 55), where instructions count: 430 a thread, a quarter of them for the angle, and
+// as many for the conversions.
 constexpr int kAppendThreads = 128;
 constexpr int kAppendElements = 16 * kAppendThreads;        // of K in a CTA: several rows, or some heads of one
 constexpr int kAppendMaxRows = 16;
