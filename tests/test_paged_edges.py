@@ -192,8 +192,8 @@ def _one_page_each(k, hq, hkv, d, page, sharing, seed):
     pools = [torch.randn((firsts + k, hkv, page, d), device="cuda", dtype=BF16, generator=g) for _ in range(2)]
     lengths = torch.randint(page, 2 * page, (k,), dtype=torch.int32, device="cuda", generator=g)
     lengths[::97] = -1
-    q, kn, vn = (torch.randn((k, h, d), device="cuda", dtype=BF16, generator=g) for h in (hq, hkv, hkv))
-    return PagedCaches(*pools, table), lengths, q, kn, vn
+    new = torch.randn((k, hq + 2 * hkv, d), device="cuda", dtype=BF16, generator=g)          # (as a fused projection leaves them)
+    return PagedCaches(*pools, table), lengths, new[:, :hq], new[:, hq:hq + hkv], new[:, hq + hkv:]
 
 
 def _check_every_prompt(caches, n_rows, q, out, shared):
@@ -384,7 +384,7 @@ def test_captured_step_is_the_step(prompts, sharing, hq, hkv, d):
     starts = list(range(0, prompts, sharing or prompts)) + [prompts]
     groups = tuple(torch.tensor(x, dtype=torch.int32, device="cuda") for x in (starts, [16] * (len(starts) - 1))) if sharing else None
     dec, eager = PagedDecoder(caches, hq, 10000.0), PagedDecoder(caches, hq, 10000.0)
-    out, g = torch.zeros_like(q), torch.cuda.CUDAGraph()
+    out, g = torch.zeros_like(q, memory_format=torch.contiguous_format), torch.cuda.CUDAGraph()
     stream = torch.cuda.Stream()
     stream.wait_stream(torch.cuda.current_stream())
     with torch.cuda.stream(stream):
@@ -395,7 +395,7 @@ def test_captured_step_is_the_step(prompts, sharing, hq, hkv, d):
     for turn in range(3):
         lengths.copy_(torch.where(lengths < 0, lengths, 16 + (lengths + 5 * turn) % 16))
         for x in (q, kn, vn):
-            x.copy_(x.roll(turn + 1, 0))
+            x.copy_(x.roll(turn + 1, 0).clone())
         out.zero_()
         torch.cuda.synchronize()
         with torch.cuda.stream(stream):
