@@ -10,8 +10,8 @@
 //   warp 1       issues tcgen05.mma: S_t = Q_t K^T into TMEM, O_t += P_t V with P_t read from TMEM, for the two row tiles t
 //   warps 2-3    TMA-load Q of tile 0 / 1, as two bf16 numbers, which the products add up: one alone moves O by as much as its last
 //                rounding does (against 64 bits, O's last rounding being 1.7e-3 of it: 16 samples of a prompt of 2000 rows 2.7e-3 with
-//                one, 2.1e-3 with two, 22.0 and 22.3 us; 24 prompts of 8 samples 2.6e-3 and 2.1e-3, 178 and 190; 64 prompts behind 32 700
-//                rows, heads of 64, 2.9e-3 and 2.3e-3, 52.4 and 52.8; 256 prompts behind 8200 rows 2.9e-3 and 2.3e-3, 112 and 119).
+//                one, 2.1e-3 with two, 22.0 and 22.3 us; 24 prompts of 8 samples 2.6e-3 and 2.1e-3, 178 and 193; 64 prompts behind 32 700
+//                rows, heads of 64, 2.9e-3 and 2.3e-3, 52.4 and 52.8; 256 prompts behind 8200 rows 2.9e-3 and 2.3e-3, 113 and 120).
 //                P is one bf16 number: two would double the conversions of the softmax, which bounds, and P V.
 //   warps 4-7    softmax of tile 0, a thread per row: no row is split between threads, so nothing is exchanged
 //   warps 8-11   the same for tile 1
@@ -47,7 +47,7 @@ template <int D> struct SharedCfg {
   static constexpr int kMiscBytes = 1024;
   // Tile t's part x of Q lies at (2 t + x) kQBytes, and behind the queries the ring. Both parts of both tiles leave it three stages with
   // heads of 128. Where no group has more than 128 queries for a KV head, nothing needs the second tile's room, and it has five (24 prompts
-  // of 8 samples, 32 heads of 128: 190 us with five, 204 with three).
+  // of 8 samples, 32 heads of 128: 190 to 194 us with five, 204 with three).
   static constexpr int kSlots = D == 128 ? 7 : 14;
   static constexpr int kStages = D == 128 ? 5 : 10, kWideStages = D == 128 ? 3 : 10;
   static __device__ __forceinline__ uint32_t q_at(uint32_t t, uint32_t part) { return (2u * t + part) * (uint32_t)kQBytes; }
